@@ -9,6 +9,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include "api_common.h"
 #include "cc_join.h"
 #include "join_internal.h"
 #include "sort_choice.h"
@@ -34,45 +35,15 @@ struct cc_store {
     int64_t map_groups;              // probe groups in d_map (a power of two)
 };
 
+using ccj::aligned;
+using ccj::device_error;
+using ccj::DeviceGuard;
+using ccj::mul_ok;
+using ccj::overlaps;
+
+thread_local int ccj::g_last_device_error = 0;
+
 namespace {
-
-thread_local int g_last_device_error = 0;
-
-cc_status device_error(hipError_t e) {
-    g_last_device_error = (int)e;
-    return CC_ERR_DEVICE;
-}
-
-bool aligned(const void *p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
-
-bool mul_ok(int64_t a, int64_t b, int64_t *r) { return !__builtin_mul_overflow(a, b, r); }
-
-bool overlaps(const void *a, int64_t na, const void *b, int64_t nb) {
-    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-    return na > 0 && nb > 0 && x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
-}
-
-// Keeps the store's device current for the duration of a call.
-class DeviceGuard {
-public:
-    explicit DeviceGuard(int dev) {
-        err_ = hipGetDevice(&prev_);
-        if (err_ == hipSuccess && prev_ != dev) {
-            err_ = hipSetDevice(dev);
-            switched_ = err_ == hipSuccess;
-        }
-    }
-    ~DeviceGuard() {
-        if (switched_)
-            (void)hipSetDevice(prev_);
-    }
-    hipError_t error() const { return err_; }
-
-private:
-    int prev_ = 0;
-    hipError_t err_ = hipSuccess;
-    bool switched_ = false;
-};
 
 cc_status join_impl(const cc_store *store, int32_t n_viewers, const int64_t *cand_offsets,
                     const int64_t *cand_idx, const int64_t *cand_author, int64_t total_cand,
@@ -252,7 +223,7 @@ void free_store(cc_store *s) {
 cc_status alloc_failure(cc_store *s, hipError_t err) {
     free_store(s);
     if (err == hipErrorOutOfMemory || err == hipErrorMemoryAllocation) {
-        g_last_device_error = (int)err;
+        ccj::g_last_device_error = (int)err;
         (void)hipGetLastError();
         return CC_ERR_OUT_OF_MEMORY;
     }
@@ -804,6 +775,6 @@ const char *cc_status_string(int status) {
     return "CC_UNKNOWN_STATUS";
 }
 
-int cc_last_device_error(void) { return g_last_device_error; }
+int cc_last_device_error(void) { return ccj::g_last_device_error; }
 
 }  // extern "C"

@@ -1,0 +1,535 @@
+"""The scoring model's input layer on the GPU against numpy in 64 bits.
+
+Tolerances. Inputs are values that their type holds, so what differs is the kernels' 32-bit
+arithmetic (half a unit each, 2^-24 relative) and the one rounding to the output's type:
+  lookup, dropout   one product by a factor that is itself rounded (2), one addition (1): 3 * 2^-24
+                    of the terms' magnitude, + half a unit of the output's type
+  grad              (additions + 2) * 2^-24 of the sum of magnitudes, + the same rounding
+  product           conversion of the sum, two products, one addition: 4 * 2^-24 of the terms'
+                    magnitude, + the same rounding
+Quantisation is compared for equality, step by step in 32 bits.
+"""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+import layers_oracle as O
+import paper_2609_22441_amd as P
+from gpu_common import note
+from layers_common import (DEV, F32, HALF_ULP, TINY, TYPES, Output, assert_close, on_gpu, rng,
+                           values)
+
+pytestmark = pytest.mark.gpu
+
+COLS = [1, 3, 7, 8, 9, 16, 96, 97, 128, 515, 1000, 1024]
+DROP = dict(p=0.3, seed=0x1234_5678_9ABC_DEF0, site=7, first_row=(1 << 33) - 2)
+
+
+def tolerance(want, terms, ops, out):
+    return ops * F32 * terms + HALF_ULP[out] * (np.abs(want) + ops * F32 * terms) + TINY[out]
+
+
+def ids_of(r, n, rows, narrow, invalid=True):
+    ids = r.integers(0, max(rows, 1), n)
+    if invalid and n > 2:
+        ids[r.integers(0, n, max(1, n // 10))] = -1
+        ids[r.integers(0, n, 1)] = rows
+        ids[r.integers(0, n, 1)] = np.iinfo(np.int32 if narrow else np.int64).min
+    return ids.astype(np.int32 if narrow else np.int64)
+
+
+# ---- lookup ----
+
+@pytest.mark.parametrize("cols", COLS)
+@pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("f16", "f16"), ("f32", "f32"),
+                                       ("f32", "bf16"), ("f32", "f16")])
+@pytest.mark.parametrize("dropped", [False, True])
+def test_lookup(cols, dtype, out, dropped):
+    note(f"lookup cols={cols} {dtype}->{out} drop={dropped}")
+    r = rng(cols)
+    rows, n = 37, 61
+    table, t = values(r, rows, cols, dtype)
+    ids = ids_of(r, n, rows, cols % 2)
+    drop = DROP if dropped else None
+    want = O.lookup(table, ids, 1.7, drop)
+    for pad, shift in ((0, 0), (8, 8), (3, 1)):
+        o = Output(n, cols, TYPES[out], pad, shift)
+        P.cc_embedding_lookup(on_gpu(t, pad, shift), torch.from_numpy(ids).to(DEV), o.t, scale=1.7,
+                              **(drop or {}))
+        assert_close(o.get(), want, tolerance(want, np.abs(want), 3, out), f"pad {pad}")
+
+
+@pytest.mark.parametrize("n,rows,cols", [(1, 1, 8), (1, 5, 4096), (3, 1, 2048), (4097, 9, 1),
+                                         (700, 50, 8191), (2100, 3, 2056), (70_000, 11, 64)])
+def test_lookup_sizes(n, rows, cols):
+    """One row to more blocks than one pass of small launches; rows longer than a tile."""
+    note(f"lookup n={n} rows={rows} cols={cols}")
+    r = rng(n)
+    table, t = values(r, rows, cols, "bf16")
+    ids = r.integers(0, rows, n)
+    o = Output(n, cols, torch.bfloat16)
+    P.cc_embedding_lookup(t.to(DEV), torch.from_numpy(ids).to(DEV), o.t)
+    assert_close(o.get(), table[ids], 0.0)
+
+
+def test_lookup_of_an_empty_table_and_of_nothing():
+    note("lookup: empty table")
+    o = Output(5, 24, torch.float32)
+    P.cc_embedding_lookup(torch.empty(0, 24, device=DEV), torch.arange(5, device=DEV), o.t)
+    assert_close(o.get(), np.zeros((5, 24)), 0.0)
+    empty = torch.empty(0, 24, device=DEV)
+    P.cc_embedding_lookup(torch.empty(3, 24, device=DEV),
+                          torch.empty(0, dtype=torch.int64, device=DEV), empty)
+
+
+def test_lookup_keeps_special_values_out_of_dropped_places():
+    note("lookup: NaN and infinities")
+    rows, cols = 6, 40
+    t = torch.full((rows, cols), float("nan"))
+    t[1::2] = float("inf")
+    ids = torch.arange(rows)
+    o = Output(rows, cols, torch.float32)
+    P.cc_embedding_lookup(t.to(DEV), ids.to(DEV), o.t, **DROP)
+    got, keep = o.get(), O.kept(rows, cols, **DROP)
+    assert (got[~keep] == 0).all()
+    assert np.isnan(got[::2][keep[::2]]).all() and np.isinf(got[1::2][keep[1::2]]).all()
+
+
+# ---- gradient ----
+
+def run_grad(ids, dout, rows, cols, table_type, accumulate=None, pad=0, shift=0, **kw):
+    n = len(ids)
+    o = Output(rows, cols, TYPES[table_type], pad, shift)
+    if accumulate is not None:
+        o.t.copy_(accumulate)
+    ws = torch.full((P.cc_embedding_grad_workspace_bytes(n, rows, cols),), 0xA5, dtype=torch.uint8,
+                    device=DEV)
+    P.cc_embedding_grad(torch.from_numpy(ids).to(DEV), on_gpu(dout, pad, shift), o.t, ws,
+                        accumulate=accumulate is not None, **kw)
+    return o.get()
+
+
+@pytest.mark.parametrize("cols", COLS)
+@pytest.mark.parametrize("dtype,table", [("bf16", "f32"), ("f32", "f32"), ("bf16", "bf16"),
+                                         ("f16", "f32"), ("f16", "f16")])
+@pytest.mark.parametrize("dropped", [False, True])
+def test_grad(cols, dtype, table, dropped):
+    note(f"grad cols={cols} {dtype}->{table} drop={dropped}")
+    r = rng(cols + 1)
+    rows, n = 41, 203
+    dout, d = values(r, n, cols, dtype)
+    ids = ids_of(r, n, rows, cols % 2)
+    drop = DROP if dropped else None
+    want, size, count = O.grad(ids, dout, rows, 0.6, drop)
+    tol = tolerance(want, size, count + 2, table)
+    for pad, shift in ((0, 0), (3, 1)):
+        got = run_grad(ids, d, rows, cols, table, pad=pad, shift=shift, scale=0.6, **(drop or {}))
+        assert_close(got, want, tol, f"pad {pad}")
+
+
+def skewed(r, n, rows, kind):
+    if kind == "one":
+        return np.full(n, rows // 2)
+    if kind == "ends":
+        return np.where(np.arange(n) % 2, 0, rows - 1)
+    if kind == "slots":
+        return np.minimum(r.integers(0, 4 * rows, n), rows - 1)
+    if kind == "none":
+        return np.full(n, -1)
+    if kind == "sorted":
+        return np.sort(r.integers(0, rows, n))
+    w = np.arange(1, rows + 1) ** -1.1
+    return r.permutation(rows)[np.searchsorted(np.cumsum(w / w.sum()), r.random(n)).clip(0, rows - 1)]
+
+
+@pytest.mark.parametrize("kind", ["one", "ends", "slots", "none", "sorted", "zipf"])
+@pytest.mark.parametrize("n,rows,cols", [(1, 1, 5), (1, 700, 40), (2, 2, 16), (64, 3, 33),
+                                         (65, 511, 8), (2_049, 512, 24), (4_096, 1, 16),
+                                         (4_097, 1_000, 100), (9_000, 70_000, 16),
+                                         (20_000, 51, 3), (5_000, 300_000, 2)])
+def test_grad_of_skewed_ids(kind, n, rows, cols):
+    """Runs that cross many chunks, tables far larger and far smaller than the call, one to three
+    digits, and rows that no id points at."""
+    note(f"grad {kind} n={n} rows={rows} cols={cols}")
+    r = rng(n + rows)
+    ids = skewed(r, n, rows, kind).astype(np.int64)
+    dout, d = values(r, n, cols, "f32")
+    want = np.zeros((rows, cols))
+    size, count = np.zeros((rows, cols)), np.zeros((rows, 1))
+    ok = ids >= 0
+    np.add.at(want, ids[ok], dout[ok])
+    np.add.at(size, ids[ok], np.abs(dout[ok]))
+    np.add.at(count, ids[ok], 1)
+    got = run_grad(ids, d, rows, cols, "f32")
+    assert_close(got, want, tolerance(want, size, count + 2, "f32"))
+
+
+@pytest.mark.parametrize("table", ["f32", "bf16"])
+def test_grad_accumulates_into_touched_rows_only(table):
+    note(f"grad accumulate {table}")
+    r = rng(5)
+    rows, cols, n = 90, 72, 300
+    ids = ids_of(r, n, rows // 2, False)
+    dout, d = values(r, n, cols, "bf16")
+    before, b = values(r, rows, cols, table)
+    want, size, count = O.grad(ids, dout, rows)
+    got = run_grad(ids, d, rows, cols, table, accumulate=b)
+    untouched = count[:, 0] == 0
+    assert (got[untouched] == before[untouched]).all()
+    tol = tolerance(want + before, size + np.abs(before), count + 3, table)
+    assert_close(got, want + before, np.where(count > 0, tol, 0.0))
+
+
+def test_grad_of_nothing():
+    note("grad: no ids, no rows")
+    none = np.empty(0, np.int64)
+    assert (run_grad(none, torch.empty(0, 40), 70, 40, "f32") == 0).all()
+    before = torch.randn(70, 40)
+    got = run_grad(none, torch.empty(0, 40), 70, 40, "f32", accumulate=before)
+    assert (got == before.double().numpy()).all()
+    ws = torch.empty(0, dtype=torch.uint8, device=DEV)
+    P.cc_embedding_grad(torch.zeros(3, dtype=torch.int64, device=DEV), torch.zeros(3, 8, device=DEV),
+                        torch.empty(0, 8, device=DEV), ws)
+
+
+def test_grad_keeps_special_values_out_of_dropped_places_and_other_rows():
+    note("grad: NaN and infinities")
+    rows, cols, n = 5, 24, 40
+    ids = np.arange(n) % rows
+    d = torch.zeros(n, cols)
+    d[ids == 2] = float("nan")
+    got = run_grad(ids, d, rows, cols, "f32", **DROP)
+    keep = O.kept(n, cols, **DROP)
+    hit = np.zeros((rows, cols), bool)
+    for t in range(n):
+        hit[ids[t]] |= keep[t] & (ids[t] == 2)
+    assert (np.isnan(got) == hit).all() and (got[~hit] == 0).all()
+
+
+def test_grad_is_the_same_every_time():
+    note("grad: repeated")
+    r = rng(8)
+    n, rows, cols = 30_000, 700, 64
+    ids = torch.from_numpy(skewed(r, n, rows, "zipf").astype(np.int64)).to(DEV)
+    d = torch.from_numpy(r.standard_normal((n, cols))).to(torch.bfloat16).to(DEV)
+    outs = []
+    for fill in (0, 0xFF, 0x3C):
+        ws = torch.full((P.cc_embedding_grad_workspace_bytes(n, rows, cols),), fill,
+                        dtype=torch.uint8, device=DEV)
+        out = torch.empty(rows, cols, device=DEV)
+        P.cc_embedding_grad(ids, d, out, ws, **DROP)
+        outs.append(out)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
+def test_grad_against_differences():
+    """The derivative of sum(w * lookup(table)) by one element of the table, from two lookups: the
+    lookup is linear, so a step of 1/4 gives it but for the rounding of the two sums."""
+    note("grad: differences")
+    r = rng(9)
+    rows, cols, n = 12, 19, 50
+    table, t = values(r, rows, cols, "f32")
+    w, wt = values(r, n, cols, "f32")
+    ids = ids_of(r, n, rows, False)
+    drop = dict(DROP, p=0.4)
+    g = run_grad(ids, wt, rows, cols, "f32", scale=1.3, **drop)
+    dev_ids = torch.from_numpy(ids).to(DEV)
+
+    def loss(x):
+        out = torch.empty(n, cols, device=DEV)
+        P.cc_embedding_lookup(x.to(DEV), dev_ids, out, scale=1.3, **drop)
+        return float((out.double().cpu() * torch.from_numpy(w)).sum())
+
+    for i, c in ((0, 0), (5, 7), (11, 18), (3, 16)):
+        up, down = t.clone(), t.clone()
+        up[i, c] += 0.25
+        down[i, c] -= 0.25
+        difference = (loss(up) - loss(down)) / 0.5
+        # each looked-up value is rounded to 24 bits: values of up to 4 * 1.3 / 0.6, 2 * 50 of them
+        bound = 100 * np.abs(w).max() * (4.3 * 1.3 / 0.6) * 3 * F32 / 0.5
+        assert abs(difference - g[i, c]) <= bound + 52 * F32 * np.abs(w).max() * 50 * 2.2
+
+
+# ---- dropout ----
+
+@pytest.mark.parametrize("cols", COLS)
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("residual", [False, True])
+def test_dropout(cols, dtype, residual):
+    note(f"dropout cols={cols} {dtype} residual={residual}")
+    r = rng(cols + 2)
+    rows = 53
+    x, t = values(r, rows, cols, dtype)
+    res, rt = values(r, rows, cols, dtype) if residual else (None, None)
+    want = O.dropout(x, DROP, res)
+    terms = np.abs(O.dropout(x, DROP)) + (0 if res is None else np.abs(res))
+    for pad, shift in ((0, 0), (8, 8), (3, 1)):
+        o = Output(rows, cols, TYPES[dtype], pad, shift)
+        P.cc_dropout(on_gpu(t, pad, shift), o.t, residual=None if rt is None else on_gpu(rt, 5),
+                     **DROP)
+        assert_close(o.get(), want, tolerance(want, terms, 3, dtype), f"pad {pad}")
+
+
+@pytest.mark.parametrize("p", [0.0, 2.0 ** -17, 2.0 ** -16, 0.5, 1 - 2.0 ** -16, 1.0])
+def test_dropout_probabilities(p):
+    note(f"dropout p={p}")
+    r = rng(3)
+    x, t = values(r, 300, 64, "f32")
+    drop = dict(DROP, p=p)
+    want = O.dropout(x, drop)
+    o = Output(300, 64, torch.float32)
+    P.cc_dropout(t.to(DEV), o.t, **drop)
+    assert_close(o.get(), want, tolerance(want, np.abs(want), 3, "f32"))
+    if p == 0:
+        assert (want == x).all()
+    if p == 1:
+        assert (want == 0).all()
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 100_003), (70_000, 8), (3, 2_056), (40_001, 33),
+                                       (5_000, 1_000)])
+def test_dropout_sizes(rows, cols):
+    note(f"dropout rows={rows} cols={cols}")
+    r = rng(rows)
+    x, t = values(r, rows, cols, "bf16")
+    drop = dict(DROP, first_row=0, site=(1 << 32) - 1)
+    want = O.dropout(x, drop)
+    o = Output(rows, cols, torch.bfloat16)
+    P.cc_dropout(t.to(DEV), o.t, **drop)
+    assert_close(o.get(), want, tolerance(want, np.abs(want), 3, "bf16"))
+
+
+def test_dropout_in_place_and_in_parts():
+    """In place on x and on the residual; rows in two parts draw the mask of the whole."""
+    note("dropout: in place, in parts")
+    r = rng(4)
+    x, t = values(r, 200, 100, "f32")
+    _, rt = values(r, 200, 100, "f32")
+    out = torch.empty(200, 100, device=DEV)
+    P.cc_dropout(t.to(DEV), out, residual=rt.to(DEV), **DROP)
+    on_x, on_res, parts = t.to(DEV), rt.to(DEV), torch.empty_like(out)
+    P.cc_dropout(on_x, on_x, residual=rt.to(DEV), **DROP)
+    P.cc_dropout(t.to(DEV), on_res, residual=on_res, **DROP)
+    for a, b in ((0, 77), (77, 200)):
+        P.cc_dropout(t[a:b].to(DEV), parts[a:b], residual=rt[a:b].to(DEV),
+                     **dict(DROP, first_row=DROP["first_row"] + a))
+    torch.cuda.synchronize()
+    assert torch.equal(on_x, out) and torch.equal(on_res, out) and torch.equal(parts, out)
+
+
+def test_dropout_keeps_special_values_out_of_dropped_places():
+    note("dropout: NaN and infinities")
+    x = torch.full((20, 40), float("nan"))
+    x[1::2] = float("-inf")
+    o = Output(20, 40, torch.bfloat16)
+    P.cc_dropout(x.to(torch.bfloat16).to(DEV), o.t, residual=torch.ones(20, 40).bfloat16().to(DEV),
+                 **DROP)
+    got, keep = o.get(), O.kept(20, 40, **DROP)
+    assert (got[~keep] == 1).all()
+    assert np.isnan(got[::2][keep[::2]]).all() and (got[1::2][keep[1::2]] == -np.inf).all()
+
+
+def test_dropout_is_the_lookups_mask():
+    """A lookup with dropout is the lookup, then dropout, on the same seed, site and rows."""
+    note("dropout: of a lookup")
+    r = rng(6)
+    _, t = values(r, 30, 72, "f32")
+    ids = torch.from_numpy(r.integers(0, 30, 90)).to(DEV)
+    both, one, two = (torch.empty(90, 72, device=DEV) for _ in range(3))
+    P.cc_embedding_lookup(t.to(DEV), ids, both, **DROP)
+    P.cc_embedding_lookup(t.to(DEV), ids, one)
+    P.cc_dropout(one, two, **DROP)
+    torch.cuda.synchronize()
+    assert torch.equal(both, two)
+
+
+def test_dropout_gradient_is_the_same_call():
+    """<dropout(x), w> = <x, dropout(w)>: the call is its own transpose; and by differences."""
+    note("dropout: gradient")
+    r = rng(7)
+    rows, cols = 40, 27
+    _, x = values(r, rows, cols, "f32")
+    w, wt = values(r, rows, cols, "f32")
+    g = torch.empty(rows, cols, device=DEV)
+    P.cc_dropout(wt.to(DEV), g, **DROP)
+    out = torch.empty_like(g)
+
+    def loss(v):
+        P.cc_dropout(v.to(DEV), out, **DROP)
+        return float((out.double().cpu() * torch.from_numpy(w)).sum())
+
+    for i, c in ((0, 0), (20, 13), (39, 26), (7, 8)):
+        up, down = x.clone(), x.clone()
+        up[i, c] += 0.25
+        down[i, c] -= 0.25
+        bound = np.abs(w[i, c]) * 6 / 0.7 * 6 * F32 / 0.5 + 1e-9    # two values rounded, x +- 1/4
+        assert abs((loss(up) - loss(down)) / 0.5 - float(g[i, c])) <= bound
+
+
+# ---- quantisation ----
+
+@pytest.mark.parametrize("cols", [1, 2, 15, 16, 17, 96, 128, 129, 512, 513, 1000, 2048, 2049, 4096,
+                                  16384, 16387, 20000])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_quantize(cols, dtype):
+    note(f"quantize cols={cols} {dtype}")
+    r = rng(cols + 3)
+    rows = 35
+    x, _ = values(r, rows, cols, dtype)
+    x *= 10.0 ** r.integers(-3, 3, (rows, 1))
+    x[3] = 0
+    t = torch.from_numpy(x).to(TYPES[dtype])
+    want_q, want_s = O.quantize(t.float().numpy())
+    padded = want_q.shape[1]
+    for pad, shift, qpad in ((0, 0, 0), (8, 8, 16), (3, 1, 32)):
+        q = Output(rows, padded, torch.int8, qpad, 0, fill=-77)
+        s = torch.full((rows,), -1.0, device=DEV)
+        P.cc_quantize_rows(on_gpu(t, pad, shift), q.t, s)
+        assert_close(q.get(), want_q.astype(np.float64), 0.0, f"q, pad {pad}")
+        assert (s.cpu().numpy() == want_s).all()
+
+
+@pytest.mark.parametrize("cols", [40, 300, 3000, 20000])
+def test_quantize_special_rows(cols):
+    """Rows of zeros, of the smallest and largest numbers, and with NaN or infinities."""
+    note(f"quantize special cols={cols}")
+    r = rng(cols)
+    x = r.standard_normal((10, cols)).astype(np.float32)
+    x[0] = 0
+    x[1] *= np.float32(2.0 ** -130)              # subnormal
+    x[2] *= np.float32(2.0 ** -62)
+    x[3] = np.where(r.random(cols) < 0.5, np.float32(3.4e38), np.float32(-3.3e38))
+    x[4, cols - 1] = np.nan
+    x[5, 0] = np.inf
+    x[6, cols // 2] = -np.inf
+    x[7] = -0.0
+    x[8] = np.float32(2.0 ** -149)
+    want_q, want_s = O.quantize(x)
+    q = Output(10, want_q.shape[1], torch.int8, fill=-77)
+    s = torch.empty(10, device=DEV)
+    P.cc_quantize_rows(torch.from_numpy(x).to(DEV), q.t, s)
+    assert_close(q.get(), want_q.astype(np.float64), 0.0)
+    got = s.cpu().numpy()
+    assert (np.isnan(got) == np.isnan(want_s)).all()
+    assert (got[~np.isnan(got)] == want_s[~np.isnan(got)]).all()
+
+
+# ---- products ----
+
+def eight_bits(r, rows, k, extreme=False):
+    padded = (k + 15) // 16 * 16
+    q = np.zeros((rows, padded), np.int8)
+    q[:, :k] = r.choice([-128, -127, 127], (rows, k)) if extreme else r.integers(-128, 128, (rows, k))
+    return q, (r.random(rows).astype(np.float32) + 0.5) / 127
+
+
+MNK = [(1, 1, 16), (1, 17, 33), (2, 64, 64), (3, 130, 1000), (5, 1030, 2055), (16, 16, 128),
+       (17, 48, 256), (31, 33, 96), (33, 257, 512), (64, 64, 4096), (65, 129, 144), (100, 515, 1040),
+       (127, 128, 128), (128, 127, 160), (129, 300, 64), (200, 256, 2048), (256, 256, 272),
+       (257, 511, 400), (333, 1030, 304), (513, 770, 48), (700, 96, 1024), (1000, 1, 96),
+       (2050, 2, 16), (1, 5000, 512), (4, 300, 16384), (640, 1280, 96)]
+
+
+@pytest.mark.parametrize("m,n,k", MNK)
+@pytest.mark.parametrize("out", ["bf16", "f16", "f32"])
+def test_product(m, n, k, out):
+    note(f"product {m}x{n}x{k} {out}")
+    r = rng(m * n + k)
+    a, sa = eight_bits(r, m, k)
+    b, sb = eight_bits(r, n, k)
+    bias = r.standard_normal(n).astype(np.float32) * 10
+    scale = 1 / np.sqrt(k)
+    sa *= np.float32(scale)
+    A, B = on_gpu(torch.from_numpy(a), 16 * (m % 2)), on_gpu(torch.from_numpy(b), 16 * (n % 3))
+    ws = torch.empty(P.cc_matmul_i8_workspace_bytes(m, n, k), dtype=torch.uint8, device=DEV)
+    args = [torch.from_numpy(v).to(DEV) for v in (sa, sb, bias)]
+    for with_bias, relu, pad, shift in ((True, True, 0, 0), (False, False, 8, 8), (True, False, 3, 1)):
+        want, size = O.product(a, sa, b, sb, bias if with_bias else None, relu)
+        o = Output(m, n, TYPES[out], pad, shift)
+        P.cc_matmul_i8(A, args[0], B, args[1], o.t, bias=args[2] if with_bias else None, relu=relu,
+                       workspace=ws)
+        assert_close(o.get(), want, tolerance(want, size, 4, out), f"bias {with_bias} relu {relu}")
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 3, 131_056), (70, 80, 131_056), (300, 270, 8192)])
+def test_product_sums_are_exact_at_the_largest_values(m, n, k):
+    """Sums close to 2^31; scales of 2^-24 make a result of up to 24 bits exact."""
+    note(f"product extreme {m}x{n}x{k}")
+    r = rng(k)
+    a, _ = eight_bits(r, m, k, extreme=True)
+    b, _ = eight_bits(r, n, k, extreme=True)
+    a[0], b[0] = -128, -128                     # the largest sum: 2^14 * k
+    one = np.ones(max(m, n), np.float32)
+    ws = torch.empty(P.cc_matmul_i8_workspace_bytes(m, n, k), dtype=torch.uint8, device=DEV)
+    o = Output(m, n, torch.float32)
+    P.cc_matmul_i8(torch.from_numpy(a).to(DEV), torch.from_numpy(one[:m]).to(DEV),
+                   torch.from_numpy(b).to(DEV), torch.from_numpy(one[:n]).to(DEV), o.t, workspace=ws)
+    want = (a.astype(np.int64) @ b.astype(np.int64).T).astype(np.float32).astype(np.float64)
+    assert_close(o.get(), want, 0.0)            # the conversion's rounding is the only one
+
+
+def test_product_of_no_columns_is_the_bias():
+    note("product k=0")
+    bias = torch.tensor([1.0, -2.0, 3.0], device=DEV)
+    empty = torch.empty(0, dtype=torch.int8, device=DEV)
+    o = Output(4, 3, torch.float32)
+    P.cc_matmul_i8(empty.view(0, 0).new_empty(4, 0), torch.ones(4, device=DEV), empty.new_empty(3, 0),
+                   torch.ones(3, device=DEV), o.t, bias=bias, relu=True)
+    assert (o.get() == np.array([[1.0, 0.0, 3.0]] * 4)).all()
+
+
+def test_product_of_nothing():
+    note("product m=0, n=0")
+    q = torch.empty(0, 32, dtype=torch.int8, device=DEV)
+    w = torch.zeros(5, 32, dtype=torch.int8, device=DEV)
+    s = torch.ones(5, device=DEV)
+    P.cc_matmul_i8(q, s[:0], w, s, torch.empty(0, 5, device=DEV))
+    P.cc_matmul_i8(w, s, q, s[:0], torch.empty(5, 0, device=DEV))
+
+
+@pytest.mark.parametrize("m,n,k", MNK)
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_linear(m, n, k, dtype):
+    note(f"linear {m}x{n}x{k} {dtype}")
+    r = rng(m + n * k)
+    x, t = values(r, m, k, dtype)
+    w, sw = eight_bits(r, n, k)
+    sw *= np.float32(1 / np.sqrt(k))
+    bias = r.standard_normal(n).astype(np.float32)
+    q, sq = O.quantize(t.float().numpy())
+    ws = torch.full((P.cc_linear_i8_workspace_bytes(m, n, k),), 0xA5, dtype=torch.uint8, device=DEV)
+    W, SW, BIAS = (torch.from_numpy(v).to(DEV) for v in (w, sw, bias))
+    for with_bias, relu, pad, shift in ((True, True, 0, 0), (False, False, 3, 1)):
+        want, size = O.product(q, sq, w, sw, bias if with_bias else None, relu)
+        o = Output(m, n, TYPES[dtype], pad, shift)
+        P.cc_linear_i8(on_gpu(t, pad, shift), W, SW, o.t, bias=BIAS if with_bias else None, relu=relu,
+                       workspace=ws)
+        assert_close(o.get(), want, tolerance(want, size, 4, dtype), f"bias {with_bias}")
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 40, 100), (9, 70, 96), (150, 300, 500), (300, 64, 96)])
+def test_linear_of_rows_that_are_not_finite(m, n, k):
+    """A row with a NaN or an infinity gives a row of NaN, with ReLU too, and no other row changes."""
+    note(f"linear not finite {m}x{n}x{k}")
+    r = rng(m)
+    x, t = values(r, m, k, "f32")
+    t[0, k - 1] = float("nan")
+    if m > 5:
+        t[5, 0] = float("-inf")
+    w, sw = eight_bits(r, n, k)
+    q, sq = O.quantize(t.numpy())
+    with np.errstate(invalid="ignore"):
+        want, size = O.product(q, sq, w, sw, None, True)
+    bad = [0] + ([5] if m > 5 else [])
+    assert np.isnan(want[bad]).all()
+    o = Output(m, n, torch.float32)
+    ws = torch.empty(P.cc_linear_i8_workspace_bytes(m, n, k), dtype=torch.uint8, device=DEV)
+    P.cc_linear_i8(t.to(DEV), torch.from_numpy(w).to(DEV), torch.from_numpy(sw).to(DEV), o.t,
+                   relu=True, workspace=ws)
+    got = o.get()
+    assert np.isnan(got[bad]).all()
+    rest = [i for i in range(m) if i not in bad]
+    assert_close(got[rest], want[rest], tolerance(want[rest], size[rest], 4, "f32"))

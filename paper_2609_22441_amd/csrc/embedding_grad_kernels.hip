@@ -212,7 +212,7 @@ __device__ __forceinline__ void write_row(const GradArgs &a, uint32_t key, int c
         const Raw<T> old = count == kCols ? load_block(p) : load_block(p, count);
 #pragma unroll
         for (int i = 0; i < kCols; ++i)
-            y[i] += (float)old.v[i];
+            y[i] += (float)old[i];
     }
     if (count == kCols)
         store_block(p, y);
@@ -308,7 +308,7 @@ __global__ __launch_bounds__(256) void sum_kernel(GradArgs a, Runs r, int64_t su
                 bits = draw_bits(a.mask, p[j].token, block);
 #pragma unroll
             for (int k = 0; k < kCols; ++k) {
-                const float v = (float)x[j].v[k];
+                const float v = (float)x[j][k];
                 sum[k] += !DROP || bits.kept(k, a.mask.threshold) ? v : 0.0f;
             }
         }
@@ -348,7 +348,7 @@ __global__ __launch_bounds__(256) void join_kernel(GradArgs a, Runs r) {
             const Raw<float> x = load_block(r.partial + (d * 2 + (d == c ? 1 : 0)) * r.width + col);
 #pragma unroll
             for (int k = 0; k < kCols; ++k)
-                sum[k] += x.v[k];
+                sum[k] += x[k];
         }
     __shared__ float part[256][kCols + 1];
 #pragma unroll

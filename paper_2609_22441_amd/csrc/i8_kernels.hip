@@ -57,7 +57,7 @@ __global__ __launch_bounds__(kThreads) void quantize_kernel(QuantizeArgs a) {
                                         : load_block(x + b * kCols, count);
 #pragma unroll
         for (int i = 0; i < kCols; ++i)
-            most = max(most, __float_as_uint((float)r.v[i]) & 0x7fffffffu);
+            most = max(most, __float_as_uint((float)r[i]) & 0x7fffffffu);
     }
 #pragma unroll
     for (int s = 1; s < (L < 64 ? L : 64); s <<= 1)
@@ -81,7 +81,7 @@ __global__ __launch_bounds__(kThreads) void quantize_kernel(QuantizeArgs a) {
         float v[kCols];
 #pragma unroll
         for (int i = 0; i < kCols; ++i)
-            v[i] = (float)r.v[i];
+            v[i] = (float)r[i];
         *(uint64_t *)(q + b * kCols) = eight_bits(v, s);
     }
 }

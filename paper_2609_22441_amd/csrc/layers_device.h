@@ -14,8 +14,20 @@ namespace {
 typedef _Float16 half_t;
 typedef __bf16 bf16_t;
 
+typedef uint32_t words_t __attribute__((ext_vector_type(4), aligned(2)));   // aligned or not
+
 constexpr int kCols = 8;         // columns of a block: one thread's unit of work, and as many as
                                  // one draw of dropout's generator serves
+
+// What no part of a launch writes, so that a wavefront whose lanes all read one place of it can do so
+// through the scalar cache.
+template <typename T>
+using Constant = const __attribute__((address_space(4))) T *;
+
+template <typename T>
+__device__ __forceinline__ Constant<T> constant(const void *p) {
+    return (Constant<T>)(uintptr_t)p;
+}
 
 // Number of column blocks in a row.
 inline __host__ __device__ int blocks_of(int cols) { return (cols + kCols - 1) / kCols; }
@@ -35,36 +47,71 @@ struct Divider {
     __device__ uint32_t operator()(uint32_t n) const { return (uint32_t)(((uint64_t)n * m) >> s); }
 };
 
-// Eight consecutive elements in 32 bits, from memory aligned to one element (the wide loads that
-// come of it need no more on this architecture) or, of a row's last block, the first `count`.
+// Eight consecutive elements, from memory aligned to one element: the wide loads that come of it need
+// no more on this architecture. Kept as words until they are used, so that several loads are in
+// flight together.
 template <typename T>
 struct Raw {
-    T v[kCols];
+    static constexpr int kWords = kCols * sizeof(T) / 16;
+    words_t w[kWords];
+    __device__ T operator[](int i) const {
+        T v[16 / sizeof(T)];
+        __builtin_memcpy(v, &w[i / (16 / sizeof(T))], 16);
+        return v[i % (16 / sizeof(T))];
+    }
 };
 
 template <typename T>
 __device__ __forceinline__ Raw<T> load_block(const T *p) {
     Raw<T> r;
-    __builtin_memcpy(&r, p, sizeof(r));
+#pragma unroll
+    for (int i = 0; i < Raw<T>::kWords; ++i)
+        r.w[i] = ((const words_t *)p)[i];
+    return r;
+}
+
+// The first `count` elements of a row's last block, then zeros.
+template <typename T>
+__device__ __forceinline__ Raw<T> load_block(const T *p, int count) {
+    T v[kCols];
+#pragma unroll
+    for (int i = 0; i < kCols; ++i)
+        v[i] = i < count ? p[i] : (T)0.0f;
+    Raw<T> r;
+    __builtin_memcpy(&r, v, sizeof(r));
     return r;
 }
 
 template <typename T>
-__device__ __forceinline__ Raw<T> load_block(const T *p, int count) {
-    Raw<T> r;
+__device__ __forceinline__ Raw<T> packed(const float (&x)[kCols]) {
+    typedef float floats __attribute__((ext_vector_type(kCols)));
+    typedef T values __attribute__((ext_vector_type(kCols)));
+    floats f;
 #pragma unroll
     for (int i = 0; i < kCols; ++i)
-        r.v[i] = i < count ? p[i] : (T)0.0f;
+        f[i] = x[i];
+    const values v = __builtin_convertvector(f, values);     // in pairs
+    Raw<T> r;
+    __builtin_memcpy(&r, &v, sizeof(r));
     return r;
 }
 
 template <typename T>
 __device__ __forceinline__ void store_block(T *p, const float (&x)[kCols]) {
-    Raw<T> r;
+    const Raw<T> r = packed<T>(x);
 #pragma unroll
-    for (int i = 0; i < kCols; ++i)
-        r.v[i] = (T)x[i];
-    __builtin_memcpy(p, &r, sizeof(r));
+    for (int i = 0; i < Raw<T>::kWords; ++i)
+        ((words_t *)p)[i] = r.w[i];
+}
+
+// The same past the caches' reach, for outputs that would push out of the caches what the kernel
+// reads more than once.
+template <typename T>
+__device__ __forceinline__ void stream_block(T *p, const float (&x)[kCols]) {
+    const Raw<T> r = packed<T>(x);
+#pragma unroll
+    for (int i = 0; i < Raw<T>::kWords; ++i)
+        __builtin_nontemporal_store(r.w[i], (words_t *)p + i);
 }
 
 template <typename T>
@@ -73,6 +120,11 @@ __device__ __forceinline__ void store_block(T *p, const float (&x)[kCols], int c
     for (int i = 0; i < kCols; ++i)
         if (i < count)
             p[i] = (T)x[i];
+}
+
+// a ^ b ^ c in one instruction: of the truth table's inputs, 0x96 has the odd ones.
+__device__ __forceinline__ uint32_t xor3(uint32_t a, uint32_t b, uint32_t c) {
+    return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96);
 }
 
 // Philox4x32-10 (Salmon et al., SC 2011): ten rounds of two 32x32 -> 64 bit products. The four
@@ -93,8 +145,8 @@ __device__ __forceinline__ Bits draw_bits(const Mask &m, int64_t row, uint32_t b
 #pragma unroll
     for (int i = 0; i < 10; ++i) {
         const uint64_t a = (uint64_t)0xD2511F53u * c0, b = (uint64_t)0xCD9E8D57u * c2;
-        c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
-        c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+        c0 = xor3((uint32_t)(b >> 32), c1, k0);
+        c2 = xor3((uint32_t)(a >> 32), c3, k1);
         c1 = (uint32_t)b;
         c3 = (uint32_t)a;
         k0 += 0x9E3779B9u;

@@ -10,7 +10,9 @@
 //          of lanes adds a chunk's rows in 32 bits, run by run; a run that lies inside the chunk is
 //          finished and written, one that crosses an edge of it is kept as a partial sum. Further
 //          workgroups of the same launch write zeros into the rows that no id points at.
-//   join   the partial sums of each run that crosses edges are added in the order of the chunks.
+//   fold   the same once more, with the partial sums of kFold chunks in the tokens' place: an id with
+//          tens of thousands of tokens leaves hundreds of them. Left out where few are possible.
+//   join   what crosses edges still is added up, one workgroup a run, in the order of the chunks.
 //
 // The work is bound by the bytes of grad_out and grad_table: pairs are 8 bytes a token, partial
 // sums at most 8 bytes a column of every chunk.
@@ -32,6 +34,7 @@ constexpr int kSortWaves = kSortThreads / 64;
 constexpr int kMaxDigitBits = 9;
 constexpr int kMaxDigits = 1 << kMaxDigitBits;
 constexpr int kMinTile = 2048;          // pairs per workgroup of a digit pass
+constexpr int kClearWords = 4 * kSortThreads;   // of 16 bytes, cleared by a workgroup
 constexpr int kMaxTiles = 256;          // every workgroup reads the counts of all tiles
 constexpr int64_t kMaxChunks = 1 << 18; // chunks times column tiles: the joins' grid stays launchable
 
@@ -72,11 +75,20 @@ struct FromPairs {
     __device__ Pair operator()(int64_t i) const { return p[i]; }
 };
 
-// Counts of each digit value in every tile: counts[tile][digit].
+// Counts of each digit value in every tile: counts[tile][digit]. The first pass's launch has further
+// workgroups that clear `found`, a byte for every row of the table.
 template <typename Source>
 __global__ __launch_bounds__(kSortThreads) void digit_counts(Source source, int64_t n, int64_t tile,
-                                                             int shift, int digits,
-                                                             uint32_t *counts) {
+                                                             int shift, int digits, int tiles,
+                                                             uint32_t *counts, words_t *found,
+                                                             int64_t found_words) {
+    if ((int)blockIdx.x >= tiles) {
+        const int64_t first = (int64_t)((int)blockIdx.x - tiles) * kClearWords;
+        const int64_t last = min(found_words, first + kClearWords);
+        for (int64_t i = first + threadIdx.x; i < last; i += kSortThreads)
+            found[i] = words_t{};
+        return;
+    }
     __shared__ uint32_t hist[kMaxDigits];
     for (int d = threadIdx.x; d < digits; d += kSortThreads)
         hist[d] = 0;
@@ -117,7 +129,7 @@ __global__ __launch_bounds__(kSortThreads) void digit_scatter(Source source, int
                                                               int64_t tile, int shift,
                                                               int digit_bits,
                                                               const uint32_t *counts, int tiles,
-                                                              Pair *out) {
+                                                              Pair *out, uint8_t *found) {
     __shared__ uint32_t place[kSortWaves][kMaxDigits];     // next place of a digit, by wavefront
     __shared__ uint32_t part[2][kSortThreads];             // sums over some tiles: all, earlier ones
     __shared__ uint32_t sums[kSortWaves];
@@ -183,89 +195,111 @@ __global__ __launch_bounds__(kSortThreads) void digit_scatter(Source source, int
             place[wave][d] = first + __popcll(peers);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
-        if (live)
+        if (live) {
             out[first + rank] = p;
+            if (found)
+                found[p.key] = 1;
+        }
     }
 }
 
 // ---- sums of runs ----
 
+constexpr int64_t kStripBytes = 128 << 10;
+
 struct Runs {
     const Pair *pairs;
+    const uint8_t *found;        // [rows]: an id points at the row
     float *partial;              // [chunks][2][width]: sums of the runs open at a chunk's start, end
     int64_t n, chunk, chunks;
     int32_t width;               // floats per partial row, a multiple of 8
     int32_t blocks;              // column blocks per row
     int32_t tiles;               // of 64 blocks or fewer each
+    __device__ int64_t chunk_of(int64_t group) const {
+        return tiles == 1 ? group : (int64_t)((uint32_t)group / (uint32_t)tiles);
+    }
 };
 
+constexpr int kFold = 8;         // chunks whose partial sums are added up together
+
+// A group's pairs: through the scalar cache where the group is a wavefront.
+template <int L>
+__device__ __forceinline__ auto pairs_of(const Pair *p) {
+    if constexpr (L == 64)
+        return constant<Pair>(p);
+    else
+        return p;
+}
+
 template <typename T>
-__device__ __forceinline__ void write_row(const GradArgs &a, uint32_t key, int col,
+__device__ __forceinline__ const T *grad_row(const GradArgs &a, uint32_t token) {
+    return (const T *)((const char *)a.grad + (int64_t)token * a.grad_stride);
+}
+
+template <typename T, bool TAIL>
+__device__ __forceinline__ void write_row(const GradArgs &a, uint32_t key, int col, bool quad,
                                           const float (&sum)[kCols]) {
     T *p = (T *)((char *)a.table + (int64_t)key * a.table_stride) + col;
-    const int count = min(kCols, a.cols - col);
+    const bool part = TAIL && col + kCols > a.cols;
     float y[kCols];
 #pragma unroll
     for (int i = 0; i < kCols; ++i)
         y[i] = sum[i] * a.factor;
     if (a.accumulate) {
-        const Raw<T> old = count == kCols ? load_block(p) : load_block(p, count);
+        const Raw<T> old = part ? load_block(p, a.cols - col) : load_block(p);
 #pragma unroll
         for (int i = 0; i < kCols; ++i)
             y[i] += (float)old[i];
     }
-    if (count == kCols)
+    if (part)
+        store_block(p, y, a.cols - col);
+    else if (TAIL)
         store_block(p, y);
     else
-        store_block(p, y, count);
+        stream_block(p, y, quad);
 }
 
-// Workgroups [0, sum_groups) add up chunks, a group of L lanes per chunk and tile of L column
-// blocks; the others write zeros into `strip` rows each.
+// `strips` of the workgroups write zeros into `strip` rows each, where no id points at them; the others
+// add up chunks, a group of L lanes per chunk and tile of L column blocks. The strips are spread
+// evenly over the launch, their writes between the chunks' reads.
 template <typename TG, typename TT, int L, bool DROP, bool TAIL>
-__global__ __launch_bounds__(256) void sum_kernel(GradArgs a, Runs r, int64_t sum_groups,
-                                                  int strip) {
-    if (blockIdx.x >= sum_groups) {
-        __shared__ uint8_t empty[256];
-        const int64_t row0 = (blockIdx.x - sum_groups) * strip;
-        const int count = (int)min((int64_t)strip, a.rows - row0);
-        if ((int)threadIdx.x < count) {
-            const uint32_t key = (uint32_t)(row0 + threadIdx.x);
-            int64_t lo = 0, hi = r.n;                  // the first pair whose key is not below
-            while (lo < hi) {
-                const int64_t mid = (lo + hi) >> 1;
-                if (r.pairs[mid].key < key)
-                    lo = mid + 1;
-                else
-                    hi = mid;
-            }
-            empty[threadIdx.x] = lo == r.n || r.pairs[lo].key != key;
-        }
-        __syncthreads();
-        for (int64_t i = threadIdx.x; i < (int64_t)count * r.blocks; i += 256) {
-            const int row = (int)(i / r.blocks), block = (int)(i - (int64_t)row * r.blocks);
-            if (empty[row]) {
-                TT *p = (TT *)((char *)a.table + (row0 + row) * a.table_stride) + block * kCols;
-                const float zero[kCols] = {};
+__global__ __launch_bounds__(256) void sum_kernel(GradArgs a, Runs r, uint32_t strips, int strip) {
+    const uint32_t strips_before = (uint32_t)((uint64_t)blockIdx.x * strips / gridDim.x);
+    if ((uint32_t)((uint64_t)(blockIdx.x + 1) * strips / gridDim.x) > strips_before) {
+        const int64_t row0 = (int64_t)strips_before * strip;
+        const int count = (int)min((int64_t)strip, a.rows - row0), lane = threadIdx.x & 63;
+        const uint64_t empty = __ballot(lane < count && !r.found[row0 + min(lane, count - 1)]);
+        const float zero[kCols] = {};
+        for (int row = threadIdx.x / L; row < count; row += 256 / L) {
+            if (!(empty >> row & 1))
+                continue;
+            TT *p = (TT *)((char *)a.table + (row0 + row) * a.table_stride);
+            for (int block = threadIdx.x % L; block < r.blocks; block += L) {
                 if (TAIL && (block + 1) * kCols > a.cols)
-                    store_block(p, zero, a.cols - block * kCols);
+                    store_block(p + block * kCols, zero, a.cols - block * kCols);
+                else if (TAIL)
+                    store_block(p + block * kCols, zero);
                 else
-                    store_block(p, zero);
+                    stream_block(p + block * kCols, zero, quad_of(block, a.cols));
             }
         }
         return;
     }
-    constexpr int kAhead = 8;                  // rows in flight per lane
-    const int64_t group = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
-    const int64_t c = group / r.tiles;
+    // Chunk and column tile of the group, the wavefront's where it is one.
+    const int64_t group = (int64_t)(blockIdx.x - strips_before) * (256 / L) +
+                          (L == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / L)
+                                   : threadIdx.x / L);
+    const int64_t c = r.chunk_of(group);
     const int block = (int)(group - c * r.tiles) * L + (int)(threadIdx.x % L);
     if (c >= r.chunks || block >= r.blocks)
         return;
     const int col = block * kCols;
+    const bool quad = quad_of(block, a.cols);
+    const auto pairs = pairs_of<L>(r.pairs);
     const int64_t i0 = c * r.chunk, i1 = min(r.n, i0 + r.chunk);
-    const bool head = i0 > 0 && r.pairs[i0 - 1].key == r.pairs[i0].key;
-    const bool tail = i1 < r.n && r.pairs[i1].key == r.pairs[i1 - 1].key;
-    uint32_t current = r.pairs[i0].key;
+    uint32_t current = pairs[i0].key;
+    const bool head = i0 > 0 && pairs[i0 - 1].key == current;
+    const bool tail = i1 < r.n && pairs[i1].key == pairs[i1 - 1].key;
     bool first = true;
     float sum[kCols] = {};
     auto finish = [&](bool open) {
@@ -273,47 +307,133 @@ __global__ __launch_bounds__(256) void sum_kernel(GradArgs a, Runs r, int64_t su
             if (open)
                 store_block(r.partial + (c * 2 + (first && head ? 0 : 1)) * r.width + col, sum);
             else
-                write_row<TT>(a, current, col, sum);
+                write_row<TT, TAIL>(a, current, col, quad, sum);
         }
     };
-    for (int64_t i = i0; i < i1 && r.pairs[i].key < (uint64_t)a.rows; i += kAhead) {
-        Pair p[kAhead];
-        Raw<TG> x[kAhead];
+    auto add = [&](uint32_t key, uint32_t token, Raw<TG> x) {
+        if (key != current) {
+            finish(first && head);
+            current = key;
+            first = false;
+#pragma unroll
+            for (int k = 0; k < kCols; ++k)
+                sum[k] = 0.0f;
+        }
+        load_rest<TAIL>(x, grad_row<TG>(a, token), col, a.cols, quad);
+        Bits bits;
+        if (DROP)
+            bits = draw_bits(a.mask, token, block);
+#pragma unroll
+        for (int k = 0; k < kCols; ++k) {
+            const float v = (float)x[k];
+            sum[k] += !DROP || bits.kept(k, a.mask.threshold) ? v : 0.0f;
+        }
+    };
+    // kAhead rows are added while the next kAhead are on their way; the last chunk's odd ones one by
+    // one. Ids outside the table come last and end the loop.
+    constexpr int kAhead = 4;
+    uint32_t key[2][kAhead], token[2][kAhead];
+    Raw<TG> x[2][kAhead];
+    auto fetch = [&](int s, int64_t i) {
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            key[s][j] = pairs[i + j].key;
+            token[s][j] = pairs[i + j].token;
+        }
 #pragma unroll
         for (int j = 0; j < kAhead; ++j)
-            p[j] = r.pairs[min(i + j, i1 - 1)];
+            x[s][j] = load_most<TAIL, true>(grad_row<TG>(a, token[s][j]), col, a.cols, quad);
+    };
+    const int64_t even = i0 + (i1 - i0) / (2 * kAhead) * (2 * kAhead);
+    if (i0 < even)
+        fetch(0, i0);
+    for (int64_t i = i0; i < even && key[0][0] < (uint64_t)a.rows; i += 2 * kAhead) {
+        fetch(1, i + kAhead);
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            const TG *g = (const TG *)((const char *)a.grad + (int64_t)p[j].token * a.grad_stride) +
-                          col;
-            if (TAIL && col + kCols > a.cols)
-                x[j] = load_block(g, a.cols - col);
-            else
-                x[j] = load_block(g);
+        for (int j = 0; j < kAhead; ++j)
+            add(key[0][j], token[0][j], x[0][j]);
+        if (i + 2 * kAhead < even)
+            fetch(0, i + 2 * kAhead);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+            add(key[1][j], token[1][j], x[1][j]);
+    }
+    for (int64_t i = even; i < i1 && pairs[i].key < (uint64_t)a.rows; ++i)
+        add(pairs[i].key, pairs[i].token,
+            load_most<TAIL, true>(grad_row<TG>(a, pairs[i].token), col, a.cols, quad));
+    finish((first && head) || tail);
+}
+
+// The partial sums of kFold chunks, a wavefront for 64 column blocks of them. A lane looks at one
+// of the 2 * kFold places for a partial sum; those that hold one, in order, are to this kernel what a chunk's
+// sorted tokens are to the one above, and runs that leave its chunks go to `out`.
+template <typename TT>
+__global__ __launch_bounds__(64) void fold_kernel(GradArgs a, Runs r, int tiles, float *out) {
+    static_assert(2 * kFold <= 64, "one place per lane");
+    const int64_t f = blockIdx.x / tiles;
+    const int lane = threadIdx.x;
+    const int block = (int)(blockIdx.x - f * tiles) * 64 + lane;
+    const int64_t c = f * kFold + lane / 2;
+    bool held = false, goes_on = false;
+    uint32_t key = 0;
+    if (lane < 2 * kFold && c < r.chunks) {
+        const int64_t i0 = c * r.chunk, i1 = min(r.n, i0 + r.chunk);
+        const uint32_t low = r.pairs[i0].key, high = r.pairs[i1 - 1].key;
+        const bool head = i0 > 0 && r.pairs[i0 - 1].key == low;
+        goes_on = i1 < r.n && r.pairs[i1].key == high;
+        key = lane & 1 ? high : low;
+        // One that is open at the chunk's start is kept there, though it may be at the end too.
+        held = lane & 1 ? goes_on && !(head && low == high) : head;
+        held &= key < (uint64_t)a.rows;
+    }
+    uint64_t places = __ballot(held);
+    if (!places)
+        return;
+    const int last_lane = (int)min(r.chunks - f * kFold, (int64_t)kFold) * 2 - 1;
+    const bool last_open = __shfl((int)goes_on, last_lane) &&
+                           __shfl((int)(key < (uint64_t)a.rows), last_lane);
+    bool open = places & 1;                       // the run at hand began before these chunks
+    const int col = block * kCols;
+    const bool live = block < r.blocks, quad = quad_of(block, a.cols);
+    const float *from = r.partial + f * 2 * kFold * r.width + (live ? col : 0);
+    float sum[kCols] = {};
+    constexpr int kAhead = 8;
+    while (places) {
+        Raw<float> x[kAhead];
+        int place[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {        // the last one again where fewer are left
+            place[j] = places ? __builtin_ctzll(places) : j ? place[j - 1] : 0;
+            x[j] = load_block(from + (int64_t)place[j] * r.width);
+            places &= places - 1;
         }
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
-            if (i + j >= i1)
+            if (j && place[j] == place[j - 1])
                 break;
-            if (p[j].key != current) {
-                finish(first && head);
-                current = p[j].key;
-                first = false;
 #pragma unroll
-                for (int k = 0; k < kCols; ++k)
-                    sum[k] = 0.0f;
+            for (int k = 0; k < kCols; ++k)
+                sum[k] += x[j][k];
+            const uint32_t here = __shfl(key, place[j]);
+            const int next = j + 1 < kAhead && place[j + 1] != place[j] ? place[j + 1]
+                             : places                                   ? __builtin_ctzll(places)
+                                                                        : -1;
+            const uint32_t there = __shfl(key, max(next, 0));
+            if (next >= 0 && there == here)
+                continue;
+            const bool leaves = next < 0 && last_open;
+            if (live) {
+                if (open || leaves)
+                    store_block(out + (f * 2 + (open ? 0 : 1)) * r.width + col, sum);
+                else
+                    write_row<TT, true>(a, here, col, quad, sum);
             }
-            Bits bits;
-            if (DROP)
-                bits = draw_bits(a.mask, p[j].token, block);
+            open = false;
 #pragma unroll
-            for (int k = 0; k < kCols; ++k) {
-                const float v = (float)x[j][k];
-                sum[k] += !DROP || bits.kept(k, a.mask.threshold) ? v : 0.0f;
-            }
+            for (int k = 0; k < kCols; ++k)
+                sum[k] = 0.0f;
         }
     }
-    finish((first && head) || tail);
 }
 
 // A workgroup per chunk and tile of L column blocks: where a run starts in the chunk and goes on
@@ -343,6 +463,7 @@ __global__ __launch_bounds__(256) void join_kernel(GradArgs a, Runs r) {
     const int col = block * kCols;
     float sum[kCols] = {};
     if (block < r.blocks)
+#pragma unroll 8
         for (int64_t d = c + group; d <= end; d += kGroups) {
             // The run is open at its first chunk's end and at the later ones' start.
             const Raw<float> x = load_block(r.partial + (d * 2 + (d == c ? 1 : 0)) * r.width + col);
@@ -360,7 +481,7 @@ __global__ __launch_bounds__(256) void join_kernel(GradArgs a, Runs r) {
 #pragma unroll
             for (int k = 0; k < kCols; ++k)
                 sum[k] += part[g * L + lane][k];
-        write_row<TT>(a, key, col, sum);
+        write_row<TT, true>(a, key, col, quad_of(block, a.cols), sum);
     }
 }
 
@@ -372,7 +493,8 @@ struct Plan {
     SortShape sort;
     int64_t chunk, chunks;
     int32_t lanes, tiles, width;
-    int64_t counts, pairs0, pairs1, partial, bytes;      // offsets and the total size
+    int64_t folds;                                       // 0: none, the chunks are joined
+    int64_t counts, found, pairs0, pairs1, partial, folded, bytes;   // offsets, the total size
 };
 
 Plan plan(int64_t n, int64_t rows, int32_t cols) {
@@ -384,7 +506,7 @@ Plan plan(int64_t n, int64_t rows, int32_t cols) {
     p.width = blocks * kCols;
     // Chunks of 64 tokens, in which the partial sums are at most 1/16 of 16-bit rows' bytes (1/32 of
     // 32-bit ones'); shorter ones while the chip has fewer than 4 wavefronts per SIMD of them.
-    p.chunk = 64;
+    p.chunk = 32;
     while (p.chunk > 8 && n / p.chunk * p.tiles * p.lanes < 4 * 1024 * 64)
         p.chunk /= 2;
     while (n / p.chunk * p.tiles > kMaxChunks)
@@ -397,57 +519,79 @@ Plan plan(int64_t n, int64_t rows, int32_t cols) {
         return here;
     };
     p.counts = take((int64_t)p.sort.tiles << p.sort.digit_bits << 2);
+    p.found = take(rows + 1);               // the last: ids outside the table
     p.pairs0 = take(n * (int64_t)sizeof(Pair));
     p.pairs1 = take(p.sort.passes > 1 ? n * (int64_t)sizeof(Pair) : 0);
     p.partial = take(p.chunks * 2 * p.width * 4);
+    // A run's partial sums are added up by 256 / lanes groups of one workgroup: folded first where a
+    // group could get more than 64 of them.
+    p.folds = p.chunks > 64 * (256 / p.lanes) ? (p.chunks + kFold - 1) / kFold : 0;
+    p.folded = take(p.folds * 2 * p.width * 4);
     p.bytes = at;
     return p;
 }
 
 template <typename Source>
-void launch_pass(Source source, const Plan &p, int64_t n, int pass, uint32_t *counts, Pair *out,
+void launch_pass(Source source, const GradArgs &a, const Plan &p, int pass, Pair *out,
                  hipStream_t stream) {
+    char *ws = static_cast<char *>(a.workspace);
+    uint32_t *counts = (uint32_t *)(ws + p.counts);
+    uint8_t *found = pass == 0 && !a.accumulate ? (uint8_t *)(ws + p.found) : nullptr;
+    const int64_t words = found ? round16(a.rows + 1) / 16 : 0;
+    const int64_t clears = (words + kClearWords - 1) / kClearWords;
     const int shift = pass * p.sort.digit_bits;
-    digit_counts<<<p.sort.tiles, kSortThreads, 0, stream>>>(source, n, p.sort.tile, shift,
-                                                            1 << p.sort.digit_bits, counts);
-    digit_scatter<<<p.sort.tiles, kSortThreads, 0, stream>>>(source, n, p.sort.tile, shift,
-                                                             p.sort.digit_bits, counts,
-                                                             p.sort.tiles, out);
+    if (p.sort.tiles + clears > 0)
+        digit_counts<<<(unsigned)(p.sort.tiles + clears), kSortThreads, 0, stream>>>(
+            source, a.n, p.sort.tile, shift, 1 << p.sort.digit_bits, p.sort.tiles, counts,
+            (words_t *)found, words);
+    if (p.sort.tiles > 0)
+        digit_scatter<<<p.sort.tiles, kSortThreads, 0, stream>>>(
+            source, a.n, p.sort.tile, shift, p.sort.digit_bits, counts, p.sort.tiles, out, found);
 }
 
 template <typename TG, typename TT, int L, bool DROP, bool TAIL>
-void launch_sum(const GradArgs &a, const Runs &r, hipStream_t stream) {
+void launch_sum(const GradArgs &a, const Runs &r, const Plan &p, hipStream_t stream) {
     const int64_t sum_groups = (r.chunks * r.tiles + 256 / L - 1) / (256 / L);
-    // Strips of rows of about 64 KiB.
+    // Strips of rows of about 128 KiB.
     const int64_t row_bytes = (int64_t)a.cols * sizeof(TT);
-    const int strip = (int)std::max<int64_t>(1, std::min<int64_t>(256, 65536 / row_bytes));
+    const int strip = (int)std::max<int64_t>(1, std::min<int64_t>(64, kStripBytes / row_bytes));
     const int64_t strips = a.accumulate ? 0 : (a.rows + strip - 1) / strip;
     if (sum_groups + strips > 0)
         sum_kernel<TG, TT, L, DROP, TAIL><<<(unsigned)(sum_groups + strips), 256, 0, stream>>>(
-            a, r, sum_groups, strip);
-    if (r.chunks > 1)
-        join_kernel<TT, L><<<(unsigned)(r.chunks * r.tiles), 256, 0, stream>>>(a, r);
+            a, r, (uint32_t)strips, strip);
+    Runs j = r;
+    if (p.folds) {
+        j.partial = (float *)((char *)a.workspace + p.folded);
+        j.chunk = r.chunk * kFold;
+        j.chunks = p.folds;
+        const int tiles = (r.blocks + 63) / 64;
+        fold_kernel<TT><<<(unsigned)(p.folds * tiles), 64, 0, stream>>>(a, r, tiles, j.partial);
+    }
+    if (j.chunks > 1)
+        join_kernel<TT, L><<<(unsigned)(j.chunks * r.tiles), 256, 0, stream>>>(a, j);
 }
 
 template <typename TG, typename TT, int L>
-void launch_drop(const GradArgs &a, const Runs &r, hipStream_t stream) {
-    const bool drop = a.mask.threshold != kThresholdOne, tail = a.cols % kCols;
+void launch_drop(const GradArgs &a, const Runs &r, const Plan &p, hipStream_t stream) {
+    const bool drop = a.mask.threshold != kThresholdOne;
+    const bool tail = a.cols % kCols || !even_rows(a.grad, a.grad_stride) ||
+                      !even_rows(a.table, a.table_stride);
     if (drop)
-        tail ? launch_sum<TG, TT, L, true, true>(a, r, stream)
-             : launch_sum<TG, TT, L, true, false>(a, r, stream);
+        tail ? launch_sum<TG, TT, L, true, true>(a, r, p, stream)
+             : launch_sum<TG, TT, L, true, false>(a, r, p, stream);
     else
-        tail ? launch_sum<TG, TT, L, false, true>(a, r, stream)
-             : launch_sum<TG, TT, L, false, false>(a, r, stream);
+        tail ? launch_sum<TG, TT, L, false, true>(a, r, p, stream)
+             : launch_sum<TG, TT, L, false, false>(a, r, p, stream);
 }
 
 template <typename TG, typename TT>
-void launch_lanes(const GradArgs &a, const Runs &r, int lanes, hipStream_t stream) {
-    if (lanes == 4)
-        launch_drop<TG, TT, 4>(a, r, stream);
-    else if (lanes == 16)
-        launch_drop<TG, TT, 16>(a, r, stream);
+void launch_lanes(const GradArgs &a, const Runs &r, const Plan &p, hipStream_t stream) {
+    if (p.lanes == 4)
+        launch_drop<TG, TT, 4>(a, r, p, stream);
+    else if (p.lanes == 16)
+        launch_drop<TG, TT, 16>(a, r, p, stream);
     else
-        launch_drop<TG, TT, 64>(a, r, stream);
+        launch_drop<TG, TT, 64>(a, r, p, stream);
 }
 
 }  // namespace
@@ -459,31 +603,29 @@ int64_t grad_workspace_bytes(int64_t n, int64_t rows, int32_t cols) {
 hipError_t launch_embedding_grad(const GradArgs &a, hipStream_t stream) {
     const Plan p = plan(a.n, a.rows, a.cols);
     char *ws = static_cast<char *>(a.workspace);
-    uint32_t *counts = (uint32_t *)(ws + p.counts);
     Pair *pairs[2] = {(Pair *)(ws + p.pairs0), (Pair *)(ws + p.pairs1)};
-    for (int pass = 0; a.n > 0 && pass < p.sort.passes; ++pass) {
+    for (int pass = 0; pass < (a.n > 0 ? p.sort.passes : 1); ++pass) {
         Pair *out = pairs[pass & 1];
         if (pass)
-            launch_pass(FromPairs{pairs[(pass - 1) & 1]}, p, a.n, pass, counts, out, stream);
+            launch_pass(FromPairs{pairs[(pass - 1) & 1]}, a, p, pass, out, stream);
         else if (a.id_bytes == 4)
-            launch_pass(FromIds<int32_t>{(const int32_t *)a.ids, a.rows}, p, a.n, 0, counts, out,
-                        stream);
+            launch_pass(FromIds<int32_t>{(const int32_t *)a.ids, a.rows}, a, p, 0, out, stream);
         else
-            launch_pass(FromIds<int64_t>{(const int64_t *)a.ids, a.rows}, p, a.n, 0, counts, out,
-                        stream);
+            launch_pass(FromIds<int64_t>{(const int64_t *)a.ids, a.rows}, a, p, 0, out, stream);
     }
-    const Runs r{pairs[(p.sort.passes - 1) & 1], (float *)(ws + p.partial), a.n, p.chunk, p.chunks,
-                 p.width, blocks_of(a.cols), p.tiles};
+    const Runs r{pairs[(p.sort.passes - 1) & 1], (const uint8_t *)(ws + p.found),
+                 (float *)(ws + p.partial), a.n, p.chunk, p.chunks, p.width, blocks_of(a.cols),
+                 p.tiles};
     if (a.grad_type == kF32)
-        launch_lanes<float, float>(a, r, p.lanes, stream);
+        launch_lanes<float, float>(a, r, p, stream);
     else if (a.grad_type == kF16 && a.table_type == kF32)
-        launch_lanes<half_t, float>(a, r, p.lanes, stream);
+        launch_lanes<half_t, float>(a, r, p, stream);
     else if (a.grad_type == kF16)
-        launch_lanes<half_t, half_t>(a, r, p.lanes, stream);
+        launch_lanes<half_t, half_t>(a, r, p, stream);
     else if (a.table_type == kF32)
-        launch_lanes<bf16_t, float>(a, r, p.lanes, stream);
+        launch_lanes<bf16_t, float>(a, r, p, stream);
     else
-        launch_lanes<bf16_t, bf16_t>(a, r, p.lanes, stream);
+        launch_lanes<bf16_t, bf16_t>(a, r, p, stream);
     return hipGetLastError();
 }
 

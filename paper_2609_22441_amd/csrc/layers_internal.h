@@ -11,6 +11,9 @@ enum Type : int32_t { kF32 = 0, kF16 = 1, kBF16 = 2 };
 
 inline int type_bytes(int32_t t) { return t == kF32 ? 4 : 2; }
 
+// Rows that all start at a multiple of 16 bytes.
+inline bool even_rows(const void *p, int64_t stride) { return !(((uintptr_t)p | stride) & 15); }
+
 constexpr int32_t kMaxCols = 1 << 24;          // elements per row: blocks of a row fit 32 bits
 constexpr int64_t kMaxK = 131056;              // 8-bit product: 2^14 * k stays below 2^31
 constexpr int kThresholdOne = 65536;           // dropout threshold that keeps everything

@@ -27,22 +27,6 @@ struct RowLaunch {
 
 struct NoIds {};
 
-// A block of the row at p. TAIL: rows have a last block of fewer columns; its lanes read the block
-// before it first (in rows of one block nothing), so that the loads of all lanes are in flight before
-// the first of them is waited for.
-template <bool TAIL, typename T>
-__device__ __forceinline__ Raw<T> load_most(const T *p, int col, int cols) {
-    if (TAIL && cols < kCols)
-        return Raw<T>{};
-    return load_block(p + (TAIL && col + kCols > cols ? col - kCols : col));
-}
-
-template <bool TAIL, typename T>
-__device__ __forceinline__ void load_rest(Raw<T> &x, const T *p, int col, int cols) {
-    if (TAIL && col + kCols > cols)
-        x = load_block(p + col, cols - col);
-}
-
 template <bool DROP, bool RES, typename TI, typename TO>
 __device__ __forceinline__ void row_values(const RowArgs &a, const Raw<TI> &x, const Raw<TO> &res,
                                            int64_t row, uint32_t block, bool found,
@@ -59,8 +43,8 @@ __device__ __forceinline__ void row_values(const RowArgs &a, const Raw<TI> &x, c
     }
 }
 
-// ID: int32_t, int64_t, or NoIds (row t's source is row t). TAIL: cols is not a multiple of 8. U:
-// blocks per thread, whose loads are in flight together.
+// ID: int32_t, int64_t, or NoIds (row t's source is row t). TAIL: cols is not a multiple of 8, or a
+// matrix not aligned to 16 bytes. U: blocks per thread, whose loads are in flight together.
 template <typename TI, typename TO, typename ID, bool DROP, bool RES, bool TAIL, int U>
 __global__ __launch_bounds__(kRowThreads) void row_kernel(RowLaunch l) {
     const RowArgs &a = l.a;
@@ -89,15 +73,19 @@ __global__ __launch_bounds__(kRowThreads) void row_kernel(RowLaunch l) {
         }
         Raw<TI> x[U];
         Raw<TO> res[U];
+        bool quad[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int col = block[u] * kCols;
-            x[u] = load_most<TAIL>((const TI *)((const char *)a.src + src[u] * a.src_stride), col,
-                                   a.cols);
+            // Four lanes are in one row where its blocks are a multiple of four, and then all here:
+            // a tile starts at a multiple of four as well.
+            quad[u] = !(l.blocks & 3) && quad_of(block[u], a.cols);
+            x[u] = load_most<TAIL, !kIds>((const TI *)((const char *)a.src + src[u] * a.src_stride), col,
+                                   a.cols, quad[u]);
             if (RES)
-                res[u] = load_most<TAIL>(
+                res[u] = load_most<TAIL, true>(
                     (const TO *)((const char *)a.res + min(row[u], a.n - 1) * a.res_stride), col,
-                    a.cols);
+                    a.cols, quad[u]);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -105,17 +93,19 @@ __global__ __launch_bounds__(kRowThreads) void row_kernel(RowLaunch l) {
                 continue;
             const int col = block[u] * kCols;
             load_rest<TAIL>(x[u], (const TI *)((const char *)a.src + src[u] * a.src_stride), col,
-                            a.cols);
+                            a.cols, quad[u]);
             if (RES)
                 load_rest<TAIL>(res[u], (const TO *)((const char *)a.res + row[u] * a.res_stride),
-                                col, a.cols);
+                                col, a.cols, quad[u]);
             float y[kCols];
             row_values<DROP, RES>(a, x[u], res[u], row[u], block[u], found[u], y);
             TO *p = (TO *)((char *)a.out + row[u] * a.out_stride) + col;
             if (TAIL && col + kCols > a.cols)
                 store_block(p, y, a.cols - col);
-            else
+            else if (TAIL)
                 store_block(p, y);
+            else
+                stream_block(p, y, quad[u]);
         }
     }
 }
@@ -136,6 +126,7 @@ __global__ __launch_bounds__(kRowThreads) void wide_kernel(RowLaunch l) {
         if (row0 >= a.n || block >= (uint32_t)l.blocks)
             continue;
         const int col = block * kCols;
+        const bool quad = quad_of(block, a.cols);
         int64_t src[U];
         const TI *from[U];
         bool found[U];
@@ -154,28 +145,30 @@ __global__ __launch_bounds__(kRowThreads) void wide_kernel(RowLaunch l) {
         Raw<TO> res[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            x[u] = load_most<TAIL>(from[u], col, a.cols);
+            x[u] = load_most<TAIL, !kIds>(from[u], col, a.cols, quad);
             if (RES)
-                res[u] = load_most<TAIL>(
+                res[u] = load_most<TAIL, true>(
                     (const TO *)((const char *)a.res + min(row0 + u, a.n - 1) * a.res_stride), col,
-                    a.cols);
+                    a.cols, quad);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t row = row0 + u;
             if (row >= a.n)
                 break;
-            load_rest<TAIL>(x[u], from[u], col, a.cols);
+            load_rest<TAIL>(x[u], from[u], col, a.cols, quad);
             if (RES)
                 load_rest<TAIL>(res[u], (const TO *)((const char *)a.res + row * a.res_stride), col,
-                                a.cols);
+                                a.cols, quad);
             float y[kCols];
             row_values<DROP, RES>(a, x[u], res[u], row, block, found[u], y);
             TO *p = (TO *)((char *)a.out + row * a.out_stride) + col;
             if (TAIL && col + kCols > a.cols)
                 store_block(p, y, a.cols - col);
+            else if (TAIL)
+                store_block(p, y);
             else
-                stream_block(p, y);
+                stream_block(p, y, quad);
         }
     }
 }
@@ -209,8 +202,10 @@ hipError_t launch_tail(const RowArgs &a, hipStream_t stream) {
 
 template <typename TI, typename TO, typename ID, bool DROP, bool RES>
 hipError_t launch_drop(const RowArgs &a, hipStream_t stream) {
-    return a.cols % kCols ? launch_tail<TI, TO, ID, DROP, RES, true>(a, stream)
-                          : launch_tail<TI, TO, ID, DROP, RES, false>(a, stream);
+    const bool even = a.cols % kCols == 0 && even_rows(a.src, a.src_stride) &&
+                      even_rows(a.out, a.out_stride) && (!RES || even_rows(a.res, a.res_stride));
+    return even ? launch_tail<TI, TO, ID, DROP, RES, false>(a, stream)
+                : launch_tail<TI, TO, ID, DROP, RES, true>(a, stream);
 }
 
 template <typename TI, typename TO>

@@ -111,7 +111,6 @@ typedef __attribute__((address_space(3))) void lds_void;
 __device__ const int4_t kZeros = {0, 0, 0, 0};    // read in the place of columns past k
 
 constexpr int kStep = 64;                         // bytes of k per stage
-constexpr int kStages = 4;                        // in LDS; three of them on their way
 
 // s_waitcnt's operand for at most `vm` vector loads outstanding and no LDS operation.
 constexpr int wait_loads(int vm) { return (vm & 15) | (vm >> 4) << 14 | 7 << 4; }
@@ -135,7 +134,7 @@ __device__ __forceinline__ int swizzled(int row, int chunk) {
 // their operands from registers half as often as 16 x 16 x 64 ones. The weights are the first operand,
 // so that a lane holds four consecutive columns of one output row; the results pass through LDS once
 // more, to be written in whole rows of the wavefront's columns.
-template <typename TO, int TM, int TN, int WM, int WN>
+template <typename TO, int TM, int TN, int WM, int WN, int kStages>
 __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(ProductArgs p, uint32_t tiles_m,
                                                             uint32_t tiles_n) {
     constexpr int kWaves = WM * WN, kT = 64 * kWaves;
@@ -204,39 +203,56 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(ProductArgs p, ui
     const int8_t *const sa = lds + (wm * (TM / WM) + frow) * kStep;
     const int8_t *const sb = lds + (TM + wn * (TN / WN) + frow) * kStep;
     const int at[2] = {swizzled(frow & 15, lane >> 5) * 16, swizzled(frow & 15, 2 + (lane >> 5)) * 16};
-    auto multiply = [&](int stage) {
-        int4_t fa[2][kMB], fb[2][kNB];
+    int4_t fa[2][kMB], fb[2][kNB];                // of both halves of a stage
+    auto read = [&](int h, int step) {
+        const int stage = step % kStages * kStageBytes;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int j = 0; j < kNB; ++j)
+            fb[h][j] = *(const int4_t *)(sb + stage + j * 32 * kStep + at[h]);
+#pragma unroll
+        for (int i = 0; i < kMB; ++i)
+            fa[h][i] = *(const int4_t *)(sa + stage + i * 32 * kStep + at[h]);
+    };
+    auto multiply = [&](int h) {
+#pragma unroll
+        for (int i = 0; i < kMB; ++i)
 #pragma unroll
             for (int j = 0; j < kNB; ++j)
-                fb[h][j] = *(const int4_t *)(sb + stage * kStageBytes + j * 32 * kStep + at[h]);
+                acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[h][j], fa[h][i], acc[i][j], 0,
+                                                                  0, 0);
+        // One read after each of the first matrix instructions, so that none of them waits for it.
 #pragma unroll
-            for (int i = 0; i < kMB; ++i)
-                fa[h][i] = *(const int4_t *)(sa + stage * kStageBytes + i * 32 * kStep + at[h]);
+        for (int i = 0; i < kMB + kNB && i < kMB * kNB; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int i = 0; i < kMB; ++i)
-#pragma unroll
-                for (int j = 0; j < kNB; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[h][j], fa[h][i], acc[i][j],
-                                                                      0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
     };
+    // The fragments that one half's matrix instructions take are read while the other half's run; so
+    // a step begins with its first half in registers and reads into the next stage at its end.
+    if (steps >= kStages - 1)
+        __builtin_amdgcn_s_waitcnt(wait_loads((kStages - 2) * kLoads));
+    else
+        __builtin_amdgcn_s_waitcnt(wait_loads(0));
+    stage_barrier();
+    if (steps > 0)
+        read(0, 0);
     for (int step = 0; step < steps; ++step) {
-        if (step + 2 < steps)
-            __builtin_amdgcn_s_waitcnt(wait_loads(2 * kLoads));
-        else if (step + 1 < steps)
-            __builtin_amdgcn_s_waitcnt(wait_loads(kLoads));
+        if (step + kStages - 2 < steps)
+            __builtin_amdgcn_s_waitcnt(wait_loads((kStages - 3) * kLoads));
         else
             __builtin_amdgcn_s_waitcnt(wait_loads(0));
-        // Every wavefront's loads of this stage are in LDS, and the stage that is fetched next has been
-        // read by all.
+        // Every wavefront's loads of the next stage are in LDS, and the stage whose place is fetched
+        // into has been read by all.
         stage_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        read(1, step);
+        multiply(0);
         if (step + kStages - 1 < steps)
             fetch(step + kStages - 1);
-        multiply(step % kStages);
+        __builtin_amdgcn_sched_barrier(0);
+        read(0, step + 1);                        // past the last step: not used
+        multiply(1);
     }
     stage_barrier();                              // the stages' LDS now holds results
 
@@ -287,12 +303,12 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(ProductArgs p, ui
     }
 }
 
-template <typename TO, int TM, int TN, int WM, int WN>
+template <typename TO, int TM, int TN, int WM, int WN, int kStages>
 hipError_t launch_tiles(const ProductArgs &p, hipStream_t stream) {
     const int64_t tm = (p.m + TM - 1) / TM, tn = (p.n + TN - 1) / TN;
     if (tm * tn * (64 * WM * WN) > (int64_t)UINT32_MAX)
         return hipErrorInvalidConfiguration;
-    tile_kernel<TO, TM, TN, WM, WN><<<(unsigned)(tm * tn), 64 * WM * WN, 0, stream>>>(
+    tile_kernel<TO, TM, TN, WM, WN, kStages><<<(unsigned)(tm * tn), 64 * WM * WN, 0, stream>>>(
         p, (uint32_t)tm, (uint32_t)tn);
     return hipGetLastError();
 }
@@ -300,8 +316,8 @@ hipError_t launch_tiles(const ProductArgs &p, hipStream_t stream) {
 template <typename TO>
 hipError_t launch_product_type(const ProductArgs &p, hipStream_t stream) {
     if (p.m > 128 * 12 && p.n > 128 * 12)
-        return launch_tiles<TO, 256, 256, 2, 4>(p, stream);
-    return launch_tiles<TO, 128, 128, 2, 2>(p, stream);
+        return launch_tiles<TO, 256, 256, 2, 4, 4>(p, stream);
+    return launch_tiles<TO, 128, 128, 2, 2, 4>(p, stream);
 }
 
 }  // namespace

@@ -1,4 +1,5 @@
 // 8-bit integers with a scale per row: quantisation of rows, and the product of two such matrices.
+#include "i8_choice.h"
 #include "layers_device.h"
 
 namespace ccj {
@@ -7,6 +8,7 @@ namespace {
 typedef int int4_t __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
+constexpr int kSkinnyWaves = 8;
 
 // ---- quantisation ----
 
@@ -29,71 +31,119 @@ __device__ __forceinline__ RowScale row_scale(uint32_t most_bits) {
     return s;
 }
 
+// The largest magnitude of a block.
+template <typename T>
+__device__ __forceinline__ uint32_t top_of(const Raw<T> &x) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < kCols; ++i)
+        top = max(top, __float_as_uint((float)x[i]) & 0x7fffffffu);
+    return top;
+}
+
+// The largest of `LANES` lanes' numbers, in all of them.
+template <int LANES = 64>
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+#pragma unroll
+    for (int s = 1; s < LANES; s <<= 1)
+        x = max(x, __shfl_xor(x, s));
+    return x;
+}
+
 // Eight values to 8 bits. A row with a NaN or an infinity has the factor 0 and gets zeros.
-__device__ __forceinline__ uint64_t eight_bits(const float (&x)[kCols], const RowScale &s) {
+template <typename T>
+__device__ __forceinline__ uint64_t eight_bits(const Raw<T> &x, const RowScale &s) {
     uint64_t q = 0;
 #pragma unroll
     for (int i = 0; i < kCols; ++i) {
-        const int v = s.inverse == 0.0f ? 0 : (int)rintf(x[i] * s.raise * s.inverse);
+        const int v = s.inverse == 0.0f ? 0 : (int)rintf((float)x[i] * s.raise * s.inverse);
         q |= (uint64_t)(uint8_t)v << (8 * i);
     }
     return q;
 }
 
-// A group of L lanes per row (L = 16, 64 or the workgroup).
-template <typename T, int L>
+// A group of L lanes per row (L = 16, 64 or the workgroup), a lane with up to B blocks, which stay in
+// registers between the search for the largest and the rounding: one read of x, one write of q. Rows
+// longer than L * B blocks (B = 0) are read twice, the second time from the caches.
+template <typename T, int L, int B>
 __global__ __launch_bounds__(kThreads) void quantize_kernel(QuantizeArgs a) {
     __shared__ uint32_t wave_most[kThreads / 64];
-    const int64_t row = (int64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L;
     const int lane = threadIdx.x % L;
-    if (L < kThreads && row >= a.n)
-        return;
-    const T *x = (const T *)((const char *)a.x + row * a.x_stride);
     const int blocks = blocks_of(a.cols), padded = (a.cols + 15) / 16 * 2;   // blocks of 8 columns
-    uint32_t most = 0;
-    for (int b = lane; b < blocks; b += L) {
-        const int count = a.cols - b * kCols;
-        const Raw<T> r = count >= kCols ? load_block(x + b * kCols)
-                                        : load_block(x + b * kCols, count);
+    constexpr int kHeld = B ? B : 1;
+    for (int64_t row0 = (int64_t)blockIdx.x * (kThreads / L); row0 < a.n;
+         row0 += (int64_t)gridDim.x * (kThreads / L)) {
+        const int64_t row = row0 + threadIdx.x / L;
+        const bool here = row < a.n;
+        const T *x = (const T *)((const char *)a.x + min(row, a.n - 1) * a.x_stride);
+        auto value = [&](int block) {
+            const int count = a.cols - block * kCols;
+            return count >= kCols ? load_once(x + block * kCols)
+                                  : load_block(x + block * kCols, count);
+        };
+        Raw<T> held[kHeld];
+        uint32_t most = 0;
+        if (B) {
 #pragma unroll
-        for (int i = 0; i < kCols; ++i)
-            most = max(most, __float_as_uint((float)r[i]) & 0x7fffffffu);
+            for (int i = 0; i < kHeld; ++i)       // all on their way before the first is looked at
+                held[i] = lane + i * L < blocks ? value(lane + i * L) : Raw<T>{};
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i)
+                most = max(most, top_of(held[i]));
+        } else {
+#pragma unroll 4
+            for (int b = lane; b < blocks; b += L)
+                most = max(most, top_of(value(b)));
+        }
+        most = wave_max<(L < 64 ? L : 64)>(most);
+        if (L > 64) {
+            __syncthreads();
+            if ((threadIdx.x & 63) == 0)
+                wave_most[threadIdx.x >> 6] = most;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < kThreads / 64; ++w)
+                most = max(most, wave_most[w]);
+        }
+        if (!here)
+            continue;
+        const RowScale s = row_scale(most);
+        if (lane == 0)
+            a.scales[row] = s.scale;
+        uint64_t *q = (uint64_t *)(a.q + row * a.q_stride);
+        if (B) {
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i)
+                if (lane + i * L < padded)
+                    q[lane + i * L] = eight_bits(held[i], s);
+        } else {
+            for (int b = lane; b < padded; b += L)
+                q[b] = eight_bits(value(b), s);
+        }
     }
-#pragma unroll
-    for (int s = 1; s < (L < 64 ? L : 64); s <<= 1)
-        most = max(most, __shfl_xor(most, s));
-    if (L > 64) {
-        if ((threadIdx.x & 63) == 0)
-            wave_most[threadIdx.x >> 6] = most;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < kThreads / 64; ++w)
-            most = max(most, wave_most[w]);
-    }
-    const RowScale s = row_scale(most);
-    if (lane == 0)
-        a.scales[row] = s.scale;
-    int8_t *q = a.q + row * a.q_stride;
-    for (int b = lane; b < padded; b += L) {
-        const int count = a.cols - b * kCols;
-        const Raw<T> r = count >= kCols ? load_block(x + b * kCols)
-                                        : load_block(x + b * kCols, count);
-        float v[kCols];
-#pragma unroll
-        for (int i = 0; i < kCols; ++i)
-            v[i] = (float)r[i];
-        *(uint64_t *)(q + b * kCols) = eight_bits(v, s);
-    }
+}
+
+template <typename T, int L, int B>
+void launch_quantize_rows(const QuantizeArgs &a, hipStream_t stream) {
+    const int64_t groups = (a.n + kThreads / L - 1) / (kThreads / L), most = 1 << 22;
+    quantize_kernel<T, L, B><<<(unsigned)(groups < most ? groups : most), kThreads, 0, stream>>>(a);
 }
 
 template <typename T>
 void launch_quantize_type(const QuantizeArgs &a, hipStream_t stream) {
-    if (a.cols <= 16 * kCols)
-        quantize_kernel<T, 16><<<(unsigned)((a.n + 15) / 16), kThreads, 0, stream>>>(a);
-    else if (a.cols <= 64 * kCols)
-        quantize_kernel<T, 64><<<(unsigned)((a.n + 3) / 4), kThreads, 0, stream>>>(a);
+    const int blocks = (a.cols + 15) / 16 * 2;
+    if (blocks <= 16)
+        launch_quantize_rows<T, 16, 1>(a, stream);
+    else if (blocks <= 64)
+        launch_quantize_rows<T, 64, 1>(a, stream);
+    else if (blocks <= 128)
+        launch_quantize_rows<T, 64, 2>(a, stream);
+    else if (blocks <= 512)
+        launch_quantize_rows<T, kThreads, 2>(a, stream);
+    else if (blocks <= 2048)
+        launch_quantize_rows<T, kThreads, 8>(a, stream);
     else
-        quantize_kernel<T, kThreads><<<(unsigned)a.n, kThreads, 0, stream>>>(a);
+        launch_quantize_rows<T, kThreads, 0>(a, stream);
 }
 
 // ---- product ----
@@ -111,6 +161,7 @@ typedef __attribute__((address_space(3))) void lds_void;
 __device__ const int4_t kZeros = {0, 0, 0, 0};    // read in the place of columns past k
 
 constexpr int kStep = 64;                         // bytes of k per stage
+constexpr int kStages = 4;                        // in LDS; three of them on their way
 
 // s_waitcnt's operand for at most `vm` vector loads outstanding and no LDS operation.
 constexpr int wait_loads(int vm) { return (vm & 15) | (vm >> 4) << 14 | 7 << 4; }
@@ -134,18 +185,23 @@ __device__ __forceinline__ int swizzled(int row, int chunk) {
 // their operands from registers half as often as 16 x 16 x 64 ones. The weights are the first operand,
 // so that a lane holds four consecutive columns of one output row; the results pass through LDS once
 // more, to be written in whole rows of the wavefront's columns.
-template <typename TO, int TM, int TN, int WM, int WN, int kStages>
-__global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(ProductArgs p, uint32_t tiles_m,
+//
+// SPLIT groups of WM x WN wavefronts take every SPLIT-th stage of k each, for tiles too few to fill the
+// chip; their integer sums meet in LDS.
+template <typename TO, int TM, int TN, int WM, int WN, int SPLIT>
+__global__ __launch_bounds__(64 * WM * WN * SPLIT, 2) void tile_kernel(ProductArgs p, uint32_t tiles_m,
                                                             uint32_t tiles_n) {
-    constexpr int kWaves = WM * WN, kT = 64 * kWaves;
+    constexpr int kWaves = WM * WN, kT = 64 * kWaves;            // of a group
     constexpr int kMB = TM / WM / 32, kNB = TN / WN / 32;        // 32 x 32 blocks of a wavefront
     constexpr int kLoadsA = TM * kStep / 16 / kT, kLoadsB = TN * kStep / 16 / kT;
     constexpr int kLoads = kLoadsA + kLoadsB;
     constexpr int kStageBytes = (TM + TN) * kStep;
     // A wavefront's results of 32 rows, 16 bytes more per row against bank conflicts.
     constexpr int kPitch = kNB * 32 * sizeof(TO) + 16;
-    static_assert(kLoadsA >= 1 && kLoadsB >= 1 && 32 * kPitch * kWaves <= kStages * kStageBytes, "");
-    __shared__ __attribute__((aligned(1024))) int8_t lds[kStages * kStageBytes];
+    constexpr int kSums = kWaves * kMB * kNB * 4096;             // bytes of a group's sums
+    static_assert(kLoadsA >= 1 && kLoadsB >= 1 && 32 * kPitch * kWaves <= kStages * kStageBytes &&
+                      (SPLIT == 1 || kSums <= kStages * kStageBytes), "");
+    __shared__ __attribute__((aligned(1024))) int8_t lds[SPLIT * kStages * kStageBytes];
     __shared__ __attribute__((aligned(16))) float scale_b[TN], bias[TN];
 
     // Workgroups go round the 8 XCDs; each gets consecutive tiles, in groups of 8 rows of tiles, so
@@ -160,28 +216,34 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(ProductArgs p, ui
     const uint32_t in = id - group * 8 * tiles_n;
     const int64_t m0 = (int64_t)(group * 8 + in % rows) * TM, n0 = (int64_t)(in / rows) * TN;
 
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % kWaves;
+    const int split = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / kWaves;
     const int wm = wave / WN, wn = wave % WN;
-    // Thread t moves 16 bytes of row t / 4 (and every kT / 4 rows on) to LDS byte 16 t.
-    const int row = threadIdx.x >> 2, chunk = swizzled(row & 15, threadIdx.x & 3);
+    // Thread t of a group moves 16 bytes of row t / 4 (and every kT / 4 rows on) to LDS byte 16 t.
+    const int row = (threadIdx.x % kT) >> 2, chunk = swizzled(row & 15, threadIdx.x & 3);
     const int8_t *from[kLoads];
 #pragma unroll
     for (int i = 0; i < kLoadsA; ++i)             // rows past the last repeat it: not written
-        from[i] = p.a + min(m0 + row + i * (kT / 4), p.m - 1) * p.a_stride + chunk * 16;
+        from[i] = p.a + min(m0 + row + i * (kT / 4), p.m - 1) * p.a_stride + chunk * 16 +
+                  split * kStep;
 #pragma unroll
     for (int i = 0; i < kLoadsB; ++i)
-        from[kLoadsA + i] = p.b + min(n0 + row + i * (kT / 4), p.n - 1) * p.b_stride + chunk * 16;
-    for (int i = threadIdx.x; i < TN; i += kT) {
+        from[kLoadsA + i] = p.b + min(n0 + row + i * (kT / 4), p.n - 1) * p.b_stride + chunk * 16 +
+                            split * kStep;
+    for (int i = threadIdx.x; i < TN; i += kT * SPLIT) {
         const int64_t n = min(n0 + i, p.n - 1);
         scale_b[i] = p.b_scales[n];
         bias[i] = p.bias ? p.bias[n] : 0.0f;
     }
-    const int steps = (int)((p.k + kStep - 1) / kStep);
-    int8_t *const mine_of_stage = lds + wave * 1024;
+    // Steps of every group; the last may lie past k for some.
+    const int steps = (int)((p.k + kStep * SPLIT - 1) / (kStep * SPLIT));
+    int8_t *const stages = lds + split * kStages * kStageBytes;
     auto fetch = [&](int step) {
-        int8_t *to = mine_of_stage + (step % kStages) * kStageBytes;
-        if ((step + 1) * kStep > p.k) {           // the last one, of columns past k too
-            const bool in_k = step * kStep + chunk * 16 < p.k;
+        int8_t *to = stages + wave * 1024 + (step % kStages) * kStageBytes;
+        const int k0 = (step * SPLIT + split) * kStep;
+        if (k0 + kStep > p.k) {                   // the last one, of columns past k too
+            const bool in_k = k0 + chunk * 16 < p.k;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i)
                 from[i] = in_k ? from[i] : (const int8_t *)&kZeros;
@@ -190,7 +252,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(ProductArgs p, ui
         for (int i = 0; i < kLoads; ++i) {
             const int at = i < kLoadsA ? i * kT * 16 : TM * kStep + (i - kLoadsA) * kT * 16;
             __builtin_amdgcn_global_load_lds((global_void *)from[i], (lds_void *)(to + at), 16, 0, 0);
-            from[i] += kStep;
+            from[i] += kStep * SPLIT;
         }
     };
     int16_tile acc[kMB][kNB] = {};
@@ -200,8 +262,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(ProductArgs p, ui
             fetch(s);
     // A fragment: lane l holds 16 bytes of row l % 32, chunk l / 32 of a half of the stage's k.
     const int frow = lane & 31;
-    const int8_t *const sa = lds + (wm * (TM / WM) + frow) * kStep;
-    const int8_t *const sb = lds + (TM + wn * (TN / WN) + frow) * kStep;
+    const int8_t *const sa = stages + (wm * (TM / WM) + frow) * kStep;
+    const int8_t *const sb = stages + (TM + wn * (TN / WN) + frow) * kStep;
     const int at[2] = {swizzled(frow & 15, lane >> 5) * 16, swizzled(frow & 15, 2 + (lane >> 5)) * 16};
     int4_t fa[2][kMB], fb[2][kNB];                // of both halves of a stage
     auto read = [&](int h, int step) {
@@ -255,6 +317,32 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(ProductArgs p, ui
         multiply(1);
     }
     stage_barrier();                              // the stages' LDS now holds results
+    if constexpr (SPLIT > 1) {
+        if (split)
+#pragma unroll
+            for (int b = 0; b < kMB * kNB; ++b)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    *(int4_t *)(stages + ((wave * kMB * kNB + b) * 4 + g) * 1024 + lane * 16) =
+                        int4_t{acc[b / kNB][b % kNB][4 * g], acc[b / kNB][b % kNB][4 * g + 1],
+                               acc[b / kNB][b % kNB][4 * g + 2], acc[b / kNB][b % kNB][4 * g + 3]};
+        __syncthreads();
+        if (split)
+            return;
+#pragma unroll
+        for (int s = 1; s < SPLIT; ++s)
+#pragma unroll
+            for (int b = 0; b < kMB * kNB; ++b)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int4_t v = *(const int4_t *)(stages + s * kStages * kStageBytes +
+                                                       ((wave * kMB * kNB + b) * 4 + g) * 1024 +
+                                                       lane * 16);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        acc[b / kNB][b % kNB][4 * g + r] += v[r];
+                }
+    }
 
     int8_t *mine = lds + wave * 32 * kPitch;
     const int64_t wave_m = m0 + wm * (TM / WM), wave_n = n0 + wn * (TN / WN);
@@ -303,21 +391,134 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(ProductArgs p, ui
     }
 }
 
-template <typename TO, int TM, int TN, int WM, int WN, int kStages>
+// Few results: the weights' bytes are the work, and the way to fast ones is many loads in flight. A
+// workgroup has 16 x 16 results and its 8 wavefronts share out k, in slabs of 256 bytes; fragments come
+// from memory to registers as the matrix instruction takes them (lane l: row l % 16). The sum over k
+// may take its products in any order, so lane l's four pieces of a slab are 64 bytes in a row, and
+// four lanes read 256. The wavefronts' sums meet in LDS.
+//
+// QUANT: the rows of a (at most 16) are quantised from x in the kernel, by every workgroup again: a few
+// KiB from L2 on the weights' way, against a launch of their own.
+template <typename TO, bool QUANT>
+__global__ __launch_bounds__(64 * kSkinnyWaves) void skinny_kernel(ProductArgs p, LinearArgs x) {
+    constexpr int kSlab = 256, kT = 64 * kSkinnyWaves;
+    extern __shared__ __attribute__((aligned(16))) int8_t quantized[];     // rows of k + 16 bytes
+    __shared__ __attribute__((aligned(16))) int part[kSkinnyWaves][256];
+    __shared__ uint32_t most[16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t tiles_n = (uint32_t)((p.n + 15) / 16);
+    const int64_t m0 = (int64_t)(blockIdx.x / tiles_n) * 16, n0 = (int64_t)(blockIdx.x % tiles_n) * 16;
+    const int k = (int)p.k, piece = (lane >> 4) * 64, rows = (int)min(p.m - m0, (int64_t)16);
+    const int8_t *b = p.b + min(n0 + (lane & 15), p.n - 1) * p.b_stride;
+    const int8_t *a = QUANT ? quantized + min(lane & 15, rows - 1) * (k + 16)
+                            : p.a + (m0 + min(lane & 15, rows - 1)) * p.a_stride;
+    int4_t fb[4], fa[4];
+    // Pieces past k repeat the row's first ones; those of a count as zeros.
+    auto read = [&](const int8_t *from, int4_t (&f)[4], int k0) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const int at = k0 + piece + c * 16;
+            f[c] = *(const int4_t *)(from + (at < k ? at : 0));
+        }
+    };
+    int4_t acc = {};
+    const int first = wave * kSlab;
+    if (first < k)
+        read(b, fb, first);
+    if constexpr (QUANT) {
+        if (threadIdx.x < 16)
+            most[threadIdx.x] = 0;
+        __syncthreads();
+        const int blocks = blocks_of(x.cols), padded = k / kCols;
+        auto value = [&](int row, int block) {
+            const TO *from = (const TO *)((const char *)x.x + row * x.x_stride) + block * kCols;
+            const int count = x.cols - block * kCols;
+            return count >= kCols ? load_block(from) : load_block(from, count);
+        };
+        for (int row = 0; row < rows; ++row) {
+            uint32_t top = 0;
+            for (int block = threadIdx.x; block < blocks; block += kT)
+                top = max(top, top_of(value(row, block)));
+            top = wave_max(top);
+            if (lane == 0)
+                atomicMax(&most[row], top);
+        }
+        __syncthreads();
+        for (int row = 0; row < rows; ++row) {
+            const RowScale s = row_scale(most[row]);
+            for (int block = threadIdx.x; block < padded; block += kT)
+                *(uint64_t *)(quantized + row * (k + 16) + block * kCols) =
+                    eight_bits(value(row, block), s);
+        }
+        __syncthreads();
+    }
+    for (int k0 = first; k0 < k; k0 += kSkinnyWaves * kSlab) {
+        if (k0 != first)
+            read(b, fb, k0);
+        read(a, fa, k0);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            if (k0 + piece + c * 16 >= k)
+                fa[c] = int4_t{};
+            acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[c], fa[c], acc, 0, 0, 0);
+        }
+    }
+    *(int4_t *)&part[wave][lane * 4] = acc;
+    __syncthreads();
+    // Lane l's register r: row l % 16, column 4 (l / 16) + r.
+    if (threadIdx.x < 256) {
+        const int row = threadIdx.x >> 4, col = threadIdx.x & 15;
+        int sum = 0;
+#pragma unroll
+        for (int w = 0; w < kSkinnyWaves; ++w)
+            sum += part[w][((col >> 2) * 16 + row) * 4 + (col & 3)];
+        const int64_t m = m0 + row, n = n0 + col;
+        if (m < p.m && n < p.n) {
+            const float scale_a = QUANT ? row_scale(most[row]).scale : p.a_scales[m];
+            ((TO *)((char *)p.out + m * p.out_stride))[n] =
+                (TO)finish(sum, scale_a, p.b_scales[n], p.bias ? p.bias[n] : 0.0f, p.relu);
+        }
+    }
+}
+
+template <typename TO, int TM, int TN, int WM, int WN, int SPLIT>
 hipError_t launch_tiles(const ProductArgs &p, hipStream_t stream) {
     const int64_t tm = (p.m + TM - 1) / TM, tn = (p.n + TN - 1) / TN;
-    if (tm * tn * (64 * WM * WN) > (int64_t)UINT32_MAX)
+    if (tm * tn * (64 * WM * WN * SPLIT) > (int64_t)UINT32_MAX)
         return hipErrorInvalidConfiguration;
-    tile_kernel<TO, TM, TN, WM, WN, kStages><<<(unsigned)(tm * tn), 64 * WM * WN, 0, stream>>>(
+    tile_kernel<TO, TM, TN, WM, WN, SPLIT><<<(unsigned)(tm * tn), 64 * WM * WN * SPLIT, 0, stream>>>(
         p, (uint32_t)tm, (uint32_t)tn);
+    return hipGetLastError();
+}
+
+template <typename TO, bool QUANT>
+hipError_t launch_skinny(const ProductArgs &p, const LinearArgs &x, hipStream_t stream) {
+    const int64_t tiles = tiles_of(p.m, p.n, 16, 16);
+    skinny_kernel<TO, QUANT><<<(unsigned)tiles, 64 * kSkinnyWaves, QUANT ? p.m * (p.k + 16) : 0,
+                               stream>>>(p, x);
     return hipGetLastError();
 }
 
 template <typename TO>
 hipError_t launch_product_type(const ProductArgs &p, hipStream_t stream) {
-    if (p.m > 128 * 12 && p.n > 128 * 12)
-        return launch_tiles<TO, 256, 256, 2, 4, 4>(p, stream);
-    return launch_tiles<TO, 128, 128, 2, 2, 4>(p, stream);
+    switch (product_choice(p.m, p.n, p.k)) {
+    case kSkinny: return launch_skinny<TO, false>(p, LinearArgs{}, stream);
+    case kTile64: return launch_tiles<TO, 64, 64, 2, 2, 4>(p, stream);
+    case kTile128x64: return launch_tiles<TO, 128, 64, 2, 2, 2>(p, stream);
+    case kTile128Split: return launch_tiles<TO, 128, 128, 2, 2, 2>(p, stream);
+    case kTile128: return launch_tiles<TO, 128, 128, 2, 2, 1>(p, stream);
+    default: return launch_tiles<TO, 256, 256, 2, 4, 1>(p, stream);
+    }
+}
+
+template <typename T>
+hipError_t launch_linear_type(const LinearArgs &x, const ProductArgs &p, hipStream_t stream) {
+    if (quantize_inside(p.m, p.n, p.k))
+        return launch_skinny<T, true>(p, x, stream);
+    const QuantizeArgs q{x.x, x.q, x.scales, x.x_stride, p.a_stride, p.m, x.cols, x.type};
+    launch_quantize_type<T>(q, stream);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? launch_product_type<T>(p, stream) : e;
 }
 
 }  // namespace
@@ -330,6 +531,14 @@ hipError_t launch_quantize(const QuantizeArgs &a, hipStream_t stream) {
     else
         launch_quantize_type<bf16_t>(a, stream);
     return hipGetLastError();
+}
+
+hipError_t launch_linear(const LinearArgs &x, const ProductArgs &p, hipStream_t stream) {
+    switch (x.type) {
+    case kF32: return launch_linear_type<float>(x, p, stream);
+    case kF16: return launch_linear_type<half_t>(x, p, stream);
+    default: return launch_linear_type<bf16_t>(x, p, stream);
+    }
 }
 
 hipError_t launch_product(const ProductArgs &p, hipStream_t stream) {

@@ -277,13 +277,10 @@ cc_status cc_linear_i8(const void *x, int64_t x_stride, int32_t type, const int8
         return CC_ERR_INVALID_ARGUMENT;
     float *scales = static_cast<float *>(workspace);
     int8_t *q = static_cast<int8_t *>(workspace) + padded(4 * m);
-    const ccj::QuantizeArgs qa{x, q, scales, x_stride, padded(k), m, (int32_t)k, type};
-    hipError_t err = ccj::launch_quantize(qa, stream);
-    if (err == hipSuccess) {
-        const ccj::ProductArgs args{q, w, scales, w_scales, bias, out, padded(k), w_stride,
-                                    out_stride, m, n, padded(k), type, relu != 0};
-        err = ccj::launch_product(args, stream);
-    }
+    const ccj::LinearArgs la{x, x_stride, (int32_t)k, type, q, scales};
+    const ccj::ProductArgs args{q, w, scales, w_scales, bias, out, padded(k), w_stride, out_stride,
+                                m, n, padded(k), type, relu != 0};
+    const hipError_t err = ccj::launch_linear(la, args, stream);
     return err == hipSuccess ? CC_OK : device_error(err);
 }
 

@@ -96,6 +96,15 @@ __device__ __forceinline__ Raw<T> load_block(const T *p) {
     return r;
 }
 
+template <typename T>
+__device__ __forceinline__ Raw<T> load_once(const T *p) {
+    Raw<T> r;
+#pragma unroll
+    for (int i = 0; i < Raw<T>::kWords; ++i)
+        r.w[i] = __builtin_nontemporal_load((const words_t *)p + i);
+    return r;
+}
+
 // Where a load of a block of 32 bits takes its two words from; settle() then puts them in place.
 struct Pieces {
     int first, second;

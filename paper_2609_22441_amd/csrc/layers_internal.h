@@ -73,4 +73,14 @@ struct ProductArgs {
 };
 hipError_t launch_product(const ProductArgs &a, hipStream_t stream);
 
+// The product of rows that are quantised on the way: q, scales: room for their 8-bit form.
+struct LinearArgs {
+    const void *x;
+    int64_t x_stride;                             // bytes
+    int32_t cols, type;                           // of x; the product's k is cols rounded up to 16
+    int8_t *q;
+    float *scales;
+};
+hipError_t launch_linear(const LinearArgs &x, const ProductArgs &product, hipStream_t stream);
+
 }  // namespace ccj

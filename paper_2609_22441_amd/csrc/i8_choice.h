@@ -17,6 +17,7 @@ constexpr int32_t kTile128x64 = 2;     // 128 x 64, 2
 constexpr int32_t kTile128Split = 3;   // 128 x 128, 2
 constexpr int32_t kTile128 = 4;        // 128 x 128, 1
 constexpr int32_t kTile256 = 5;        // 256 x 256, 1
+constexpr int32_t kTileShort = 6;      // 128 x 128, 1, all of k at once
 
 constexpr int64_t kUnits = 256;        // compute units
 
@@ -30,6 +31,9 @@ constexpr int64_t kSkinnyRows = 16, kSkinnyLinearTiles = 1024, kSkinnyLds = 64 <
 
 // 512 x 8,192 x 512: 7.8 without shared k against 8.7 with it; x 2,048 16.4 / 16.0, x 8,192 48.9 / 45.4.
 constexpr int64_t kSplitK = 1024;
+
+// Of products this short the output is the work.
+constexpr int64_t kShortK = 128, kShortTile = 128;
 
 inline int64_t tiles_of(int64_t m, int64_t n, int64_t tm, int64_t tn) {
     return ((m + tm - 1) / tm) * ((n + tn - 1) / tn);
@@ -49,11 +53,17 @@ inline int32_t product_choice(int64_t m, int64_t n, int64_t k) {
     const int64_t t128 = tiles_of(m, n, 128, 128), t256 = tiles_of(m, n, 256, 256);
     if (t128 <= kUnits)
         return k >= kSplitK ? kTile128Split : kTile128;
+    if (k <= kShortK)
+        return kTileShort;
     // A unit has two 128 x 128 tiles at a time (87 for k = 8,192) or one of 256 x 256 (127): 1,024 x
     // 8,192 x 8,192 89 / 89, 2,048 x 8,192 x 8,192 127 in 256 x 256, 171 in 128 x 128.
     const int64_t r128 = (t128 + 2 * kUnits - 1) / (2 * kUnits), r256 = (t256 + kUnits - 1) / kUnits;
     return 3 * r256 <= 2 * r128 ? kTile256 : kTile128;
 }
+
+// Whether a linear layer's rows are quantised by the tile kernel: each tile of columns would do so
+// again.
+inline bool quantize_in_tile(int64_t, int64_t n, int64_t k) { return k <= kShortK && n <= kShortTile; }
 
 // Whether a linear layer's rows are quantised by the skinny kernel.
 inline bool quantize_inside(int64_t m, int64_t n, int64_t k) {

@@ -151,7 +151,7 @@ void launch_quantize_type(const QuantizeArgs &a, hipStream_t stream) {
 __device__ __forceinline__ float finish(int sum, float scale_a, float scale_b, float bias,
                                         bool relu) {
     const float y = (float)sum * scale_a * scale_b + bias;
-    return relu && y < 0.0f ? 0.0f : y;           // a NaN stays one
+    return relu ? __builtin_elementwise_maximum(y, 0.0f) : y;         // a NaN stays one
 }
 
 typedef int int16_tile __attribute__((ext_vector_type(16)));
@@ -161,7 +161,6 @@ typedef __attribute__((address_space(3))) void lds_void;
 __device__ const int4_t kZeros = {0, 0, 0, 0};    // read in the place of columns past k
 
 constexpr int kStep = 64;                         // bytes of k per stage
-constexpr int kStages = 4;                        // in LDS; three of them on their way
 
 // s_waitcnt's operand for at most `vm` vector loads outstanding and no LDS operation.
 constexpr int wait_loads(int vm) { return (vm & 15) | (vm >> 4) << 14 | 7 << 4; }
@@ -188,9 +187,17 @@ __device__ __forceinline__ int swizzled(int row, int chunk) {
 //
 // SPLIT groups of WM x WN wavefronts take every SPLIT-th stage of k each, for tiles too few to fill the
 // chip; their integer sums meet in LDS.
-template <typename TO, int TM, int TN, int WM, int WN, int SPLIT>
+//
+// With two stages k is at most both of them, and all of it is fetched at once: short products are
+// bound by their output, and a quarter of the LDS lets four workgroups overlap their loads and stores
+// on a unit.
+//
+// QUANT, of short k too and one tile of columns: the tile's rows are quantised from x on their way to
+// LDS, so that no 8-bit rows are written to memory and read back.
+template <typename TO, int TM, int TN, int WM, int WN, int SPLIT, int kStages, bool QUANT>
 __global__ __launch_bounds__(64 * WM * WN * SPLIT, 2) void tile_kernel(ProductArgs p, uint32_t tiles_m,
-                                                            uint32_t tiles_n) {
+                                                                       uint32_t tiles_n,
+                                                                       LinearArgs x) {
     constexpr int kWaves = WM * WN, kT = 64 * kWaves;            // of a group
     constexpr int kMB = TM / WM / 32, kNB = TN / WN / 32;        // 32 x 32 blocks of a wavefront
     constexpr int kLoadsA = TM * kStep / 16 / kT, kLoadsB = TN * kStep / 16 / kT;
@@ -198,11 +205,13 @@ __global__ __launch_bounds__(64 * WM * WN * SPLIT, 2) void tile_kernel(ProductAr
     constexpr int kStageBytes = (TM + TN) * kStep;
     // A wavefront's results of 32 rows, 16 bytes more per row against bank conflicts.
     constexpr int kPitch = kNB * 32 * sizeof(TO) + 16;
+    constexpr bool kWhole = kStages == 2;
+    static_assert(kWhole || (kStages >= 3 && !QUANT), "");
     constexpr int kSums = kWaves * kMB * kNB * 4096;             // bytes of a group's sums
-    static_assert(kLoadsA >= 1 && kLoadsB >= 1 && 32 * kPitch * kWaves <= kStages * kStageBytes &&
-                      (SPLIT == 1 || kSums <= kStages * kStageBytes), "");
-    __shared__ __attribute__((aligned(1024))) int8_t lds[SPLIT * kStages * kStageBytes];
-    __shared__ __attribute__((aligned(16))) float scale_b[TN], bias[TN];
+    static_assert(kLoadsA >= 1 && kLoadsB >= 1 && (SPLIT == 1 || kSums <= kStages * kStageBytes), "");
+    constexpr int kStaged = SPLIT * kStages * kStageBytes, kOutput = 32 * kPitch * kWaves;
+    __shared__ __attribute__((aligned(1024))) int8_t lds[kStaged > kOutput ? kStaged : kOutput];
+    __shared__ __attribute__((aligned(16))) float scale_b[TN], bias[TN], scale_q[QUANT ? TM : 1];
 
     // Workgroups go round the 8 XCDs; each gets consecutive tiles, in groups of 8 rows of tiles, so
     // that those it works on together share their rows of a and b in its L2.
@@ -224,7 +233,7 @@ __global__ __launch_bounds__(64 * WM * WN * SPLIT, 2) void tile_kernel(ProductAr
     const int row = (threadIdx.x % kT) >> 2, chunk = swizzled(row & 15, threadIdx.x & 3);
     const int8_t *from[kLoads];
 #pragma unroll
-    for (int i = 0; i < kLoadsA; ++i)             // rows past the last repeat it: not written
+    for (int i = 0; i < (QUANT ? 0 : kLoadsA); ++i)      // rows past the last repeat it: not written
         from[i] = p.a + min(m0 + row + i * (kT / 4), p.m - 1) * p.a_stride + chunk * 16 +
                   split * kStep;
 #pragma unroll
@@ -245,11 +254,11 @@ __global__ __launch_bounds__(64 * WM * WN * SPLIT, 2) void tile_kernel(ProductAr
         if (k0 + kStep > p.k) {                   // the last one, of columns past k too
             const bool in_k = k0 + chunk * 16 < p.k;
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i)
+            for (int i = QUANT ? kLoadsA : 0; i < kLoads; ++i)
                 from[i] = in_k ? from[i] : (const int8_t *)&kZeros;
         }
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
+        for (int i = QUANT ? kLoadsA : 0; i < kLoads; ++i) {
             const int at = i < kLoadsA ? i * kT * 16 : TM * kStep + (i - kLoadsA) * kT * 16;
             __builtin_amdgcn_global_load_lds((global_void *)from[i], (lds_void *)(to + at), 16, 0, 0);
             from[i] += kStep * SPLIT;
@@ -257,9 +266,52 @@ __global__ __launch_bounds__(64 * WM * WN * SPLIT, 2) void tile_kernel(ProductAr
     };
     int16_tile acc[kMB][kNB] = {};
 #pragma unroll
-    for (int s = 0; s < kStages - 1; ++s)
+    for (int s = 0; s < (kWhole ? kStages : kStages - 1); ++s)
         if (s < steps)
             fetch(s);
+    if constexpr (QUANT) {
+        static_assert(SPLIT == 1, "");
+        constexpr int kLanesQ = 16, kGroups = kT / kLanesQ, kRowsQ = TM / kGroups;
+        constexpr int kBlocksQ = kStages * kStep / kCols / kLanesQ;           // blocks of a lane
+        const int lane_q = threadIdx.x % kLanesQ, group_q = threadIdx.x / kLanesQ;
+        const int blocks = blocks_of(x.cols);
+        for (int r0 = 0; r0 < kRowsQ; r0 += 4) {
+            Raw<TO> held[4][kBlocksQ];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int64_t m = min(m0 + group_q + (r0 + r) * kGroups, p.m - 1);
+                const TO *of = (const TO *)((const char *)x.x + m * x.x_stride);
+#pragma unroll
+                for (int i = 0; i < kBlocksQ; ++i) {
+                    const int block = lane_q + i * kLanesQ, count = x.cols - block * kCols;
+                    held[r][i] = Raw<TO>{};
+                    if (block < blocks)
+                        held[r][i] = count >= kCols ? load_block(of + block * kCols)
+                                                    : load_block(of + block * kCols, count);
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int at_row = group_q + (r0 + r) * kGroups;
+                uint32_t most = 0;
+#pragma unroll
+                for (int i = 0; i < kBlocksQ; ++i)
+                    most = max(most, top_of(held[r][i]));
+                const RowScale s = row_scale(wave_max<kLanesQ>(most));
+                if (lane_q == 0)
+                    scale_q[at_row] = s.scale;
+#pragma unroll
+                for (int i = 0; i < kBlocksQ; ++i) {
+                    const int block = lane_q + i * kLanesQ;      // of 8 bytes; zeros past the row's
+                    if (block < steps * (kStep / kCols))
+                        *(uint64_t *)(stages + block / 8 * kStageBytes + at_row * kStep +
+                                      swizzled(at_row & 15, block % 8 / 2) * 16 + block % 2 * 8) =
+                            eight_bits(held[r][i], s);
+                }
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // before the barrier below
+    }
     // A fragment: lane l holds 16 bytes of row l % 32, chunk l / 32 of a half of the stage's k.
     const int frow = lane & 31;
     const int8_t *const sa = stages + (wm * (TM / WM) + frow) * kStep;
@@ -292,7 +344,7 @@ __global__ __launch_bounds__(64 * WM * WN * SPLIT, 2) void tile_kernel(ProductAr
     };
     // The fragments that one half's matrix instructions take are read while the other half's run; so
     // a step begins with its first half in registers and reads into the next stage at its end.
-    if (steps >= kStages - 1)
+    if (!kWhole && steps >= kStages - 1)
         __builtin_amdgcn_s_waitcnt(wait_loads((kStages - 2) * kLoads));
     else
         __builtin_amdgcn_s_waitcnt(wait_loads(0));
@@ -300,17 +352,19 @@ __global__ __launch_bounds__(64 * WM * WN * SPLIT, 2) void tile_kernel(ProductAr
     if (steps > 0)
         read(0, 0);
     for (int step = 0; step < steps; ++step) {
-        if (step + kStages - 2 < steps)
-            __builtin_amdgcn_s_waitcnt(wait_loads((kStages - 3) * kLoads));
-        else
-            __builtin_amdgcn_s_waitcnt(wait_loads(0));
-        // Every wavefront's loads of the next stage are in LDS, and the stage whose place is fetched
-        // into has been read by all.
-        stage_barrier();
+        if constexpr (!kWhole) {
+            if (step + kStages - 2 < steps)
+                __builtin_amdgcn_s_waitcnt(wait_loads((kStages - 3) * kLoads));
+            else
+                __builtin_amdgcn_s_waitcnt(wait_loads(0));
+            // Every wavefront's loads of the next stage are in LDS, and the stage whose place is
+            // fetched into has been read by all.
+            stage_barrier();
+        }
         __builtin_amdgcn_sched_barrier(0);
         read(1, step);
         multiply(0);
-        if (step + kStages - 1 < steps)
+        if (!kWhole && step + kStages - 1 < steps)
             fetch(step + kStages - 1);
         __builtin_amdgcn_sched_barrier(0);
         read(0, step + 1);                        // past the last step: not used
@@ -350,7 +404,8 @@ __global__ __launch_bounds__(64 * WM * WN * SPLIT, 2) void tile_kernel(ProductAr
 #pragma unroll
     for (int i = 0; i < kMB; ++i) {
         const int64_t m = wave_m + i * 32 + frow;
-        const float scale_a = p.a_scales[min(m, p.m - 1)];
+        const float scale_a = QUANT ? scale_q[wm * (TM / WM) + i * 32 + frow]
+                                    : p.a_scales[min(m, p.m - 1)];
 #pragma unroll
         for (int j = 0; j < kNB; ++j)
 #pragma unroll
@@ -481,13 +536,14 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void skinny_kernel(ProductArgs p
     }
 }
 
-template <typename TO, int TM, int TN, int WM, int WN, int SPLIT>
-hipError_t launch_tiles(const ProductArgs &p, hipStream_t stream) {
+template <typename TO, int TM, int TN, int WM, int WN, int SPLIT, int STAGES = 4,
+          bool QUANT = false>
+hipError_t launch_tiles(const ProductArgs &p, hipStream_t stream, const LinearArgs &x = {}) {
     const int64_t tm = (p.m + TM - 1) / TM, tn = (p.n + TN - 1) / TN;
     if (tm * tn * (64 * WM * WN * SPLIT) > (int64_t)UINT32_MAX)
         return hipErrorInvalidConfiguration;
-    tile_kernel<TO, TM, TN, WM, WN, SPLIT><<<(unsigned)(tm * tn), 64 * WM * WN * SPLIT, 0, stream>>>(
-        p, (uint32_t)tm, (uint32_t)tn);
+    tile_kernel<TO, TM, TN, WM, WN, SPLIT, STAGES, QUANT>
+        <<<(unsigned)(tm * tn), 64 * WM * WN * SPLIT, 0, stream>>>(p, (uint32_t)tm, (uint32_t)tn, x);
     return hipGetLastError();
 }
 
@@ -506,6 +562,7 @@ hipError_t launch_product_type(const ProductArgs &p, hipStream_t stream) {
     case kTile64: return launch_tiles<TO, 64, 64, 2, 2, 4>(p, stream);
     case kTile128x64: return launch_tiles<TO, 128, 64, 2, 2, 2>(p, stream);
     case kTile128Split: return launch_tiles<TO, 128, 128, 2, 2, 2>(p, stream);
+    case kTileShort: return launch_tiles<TO, 128, 128, 2, 2, 1, 2>(p, stream);
     case kTile128: return launch_tiles<TO, 128, 128, 2, 2, 1>(p, stream);
     default: return launch_tiles<TO, 256, 256, 2, 4, 1>(p, stream);
     }
@@ -515,6 +572,8 @@ template <typename T>
 hipError_t launch_linear_type(const LinearArgs &x, const ProductArgs &p, hipStream_t stream) {
     if (quantize_inside(p.m, p.n, p.k))
         return launch_skinny<T, true>(p, x, stream);
+    if (quantize_in_tile(p.m, p.n, p.k))
+        return launch_tiles<T, 128, 128, 2, 2, 1, 2, true>(p, stream, x);
     const QuantizeArgs q{x.x, x.q, x.scales, x.x_stride, p.a_stride, p.m, x.cols, x.type};
     launch_quantize_type<T>(q, stream);
     const hipError_t e = hipGetLastError();

@@ -37,7 +37,30 @@ typedef int (*upsert_fn)(cc_store *, int64_t, const int64_t *, const int64_t *, 
 typedef int (*sort_fn)(int32_t, int32_t, int32_t, const int64_t *, const int64_t *, const void *,
                        int32_t, int64_t, int64_t, int64_t *, void *, void *, int64_t, void *);
 
+/* include/cc_layers.h */
+typedef int (*lookup_fn)(const void *, int64_t, int64_t, int32_t, const void *, int32_t, int64_t,
+                         int32_t, double, double, uint64_t, uint32_t, int64_t, void *, int64_t,
+                         int32_t, void *);
+typedef int64_t (*grad_bytes_fn)(int64_t, int64_t, int32_t);
+typedef int (*grad_fn)(const void *, int32_t, int64_t, const void *, int64_t, int32_t, int32_t,
+                       double, double, uint64_t, uint32_t, int64_t, int64_t, void *, int64_t,
+                       int32_t, int32_t, void *, int64_t, void *);
+typedef int (*dropout_fn)(const void *, int64_t, const void *, int64_t, int64_t, int32_t, int32_t,
+                          double, uint64_t, uint32_t, int64_t, void *, int64_t, void *);
+typedef int (*quantize_fn)(const void *, int64_t, int32_t, int64_t, int32_t, int8_t *, int64_t,
+                           float *, void *);
+typedef int64_t (*product_bytes_fn)(int64_t, int64_t, int64_t);
+typedef int (*matmul_fn)(const int8_t *, int64_t, const float *, const int8_t *, int64_t,
+                         const float *, const float *, int64_t, int64_t, int64_t, int32_t, void *,
+                         int64_t, int32_t, void *, int64_t, void *);
+typedef int (*linear_fn)(const void *, int64_t, int32_t, const int8_t *, int64_t, const float *,
+                         const float *, int64_t, int64_t, int64_t, int32_t, void *, int64_t, void *,
+                         int64_t, void *);
+
 static PyObject *t_type, *t_i64, *t_i8;       /* torch.Tensor, torch.int64, torch.int8 */
+static PyObject *t_float[3], *t_i32;          /* by type code: torch.float32, float16, bfloat16 */
+static PyObject *get_device, *raw_stream;     /* () -> current device; (device) -> its stream */
+static PyObject *n_get_device;
 static PyObject *current_stream;              /* () -> handle of torch's current stream */
 static PyObject *n_dtype, *n_is_cuda, *n_numel, *n_contiguous, *n_data_ptr, *n_shape, *n_stride,
     *n_element_size, *n_cuda_stream;
@@ -326,6 +349,248 @@ static PyObject *m_sort(PyObject *self, PyObject *const *a, Py_ssize_t n_args) {
                        max_keys, k, r, ws, ws_bytes, stream));
 }
 
+/* ---- the scoring model's input layer (layers.py) ----
+ * As above; beyond it, every tensor is on the current device. */
+
+typedef struct {
+    void *p;
+    int64_t stride, rows, cols;               /* the row stride in bytes */
+    int32_t code;                             /* of the type: 0 to 2, or -1 for int8 */
+} Matrix;
+
+/* A tensor on device *device; the first one asked (*device < 0) says which. */
+static int on_device(PyObject *x, int64_t *device) {
+    const int64_t d = call_int(x, n_get_device);
+    if (d < 0 || (*device >= 0 && d != *device))
+        return 0;
+    *device = d;
+    return 1;
+}
+
+/* [rows, cols] with dense rows that do not overlap, of a floating-point type or (code -1) int8. */
+static int matrix_of(PyObject *x, int eight_bits, int64_t *device, Matrix *m) {
+    static const int64_t size[] = {1, 4, 2, 2};
+    int64_t step, inner;
+    if (!plain(x, NULL))
+        return 0;
+    PyObject *d = PyObject_GetAttr(x, n_dtype);
+    if (!d)
+        return not_plain();
+    m->code = d == t_i8 ? -1 : d == t_float[0] ? 0 : d == t_float[1] ? 1 : d == t_float[2] ? 2 : 3;
+    Py_DECREF(d);
+    if (m->code == 3 || (m->code < 0) != eight_bits ||
+        !pair_of(PyObject_GetAttr(x, n_shape), &m->rows, &m->cols) ||
+        !pair_of(PyObject_CallMethodNoArgs(x, n_stride), &step, &inner) ||
+        (inner != 1 && m->cols > 1) || (m->rows > 1 && step < m->cols) || !on_device(x, device))
+        return 0;
+    m->stride = (m->rows > 1 ? step : m->cols) * size[m->code + 1];
+    return m->cols <= INT32_MAX && pointer(x, &m->p);
+}
+
+static int vector_of(PyObject *x, PyObject *dtype, int64_t need, int64_t *device, void **p) {
+    return array_of(x, dtype, need, p, NULL) && on_device(x, device);
+}
+
+static int ids_of(PyObject *x, int64_t *device, void **p, int32_t *size, int64_t *n) {
+    PyObject *d = PyObject_GetAttr(x, n_dtype);
+    if (!d)
+        return not_plain();
+    *size = d == t_i64 ? 8 : d == t_i32 ? 4 : 0;
+    Py_DECREF(d);
+    return *size && array_of(x, NULL, 0, p, n) && on_device(x, device);
+}
+
+static int real(PyObject *x, double *v) {
+    if (!PyFloat_CheckExact(x) && !PyLong_CheckExact(x))
+        return 0;
+    *v = PyFloat_AsDouble(x);
+    return PyErr_Occurred() ? not_plain() : 1;
+}
+
+typedef struct {
+    double p;
+    uint64_t seed;
+    uint32_t site;
+    int64_t first_row;
+} Drop;
+
+/* a: p, seed, site, first_row */
+static int drop_of(PyObject *const *a, Drop *d) {
+    int64_t site;
+    if (!real(a[0], &d->p) || !(d->p >= 0 && d->p <= 1) || !PyLong_CheckExact(a[1]) ||
+        !number(a[2], &site) || site < 0 || site > UINT32_MAX || !number(a[3], &d->first_row) ||
+        d->first_row < 0)
+        return 0;
+    d->seed = PyLong_AsUnsignedLongLongMask(a[1]);
+    d->site = (uint32_t)site;
+    return PyErr_Occurred() ? not_plain() : 1;
+}
+
+/* The stream argument: None is the current stream of the tensors' device, which is the current one. */
+static int device_stream(PyObject *x, int64_t device, void **p) {
+    PyObject *r = PyObject_CallNoArgs(get_device);
+    if (!r)
+        return not_plain();
+    const int64_t current = PyLong_Check(r) ? PyLong_AsLongLong(r) : -1;
+    int ok = current == device && !PyErr_Occurred();
+    if (ok && x == Py_None) {
+        PyObject *h = PyObject_CallOneArg(raw_stream, r);
+        Py_DECREF(r);
+        if (!h)
+            return not_plain();
+        ok = address(h, p);
+        Py_DECREF(h);
+        return ok;
+    }
+    Py_DECREF(r);
+    return ok ? stream_of(x, p) : (PyErr_Occurred() ? not_plain() : 0);
+}
+
+static int workspace_of(PyObject *x, int64_t need, int64_t *device, void **p, int64_t *size) {
+    *p = NULL;
+    *size = 0;
+    if (x == Py_None)
+        return need == 0;
+    return bytes_of(x, need, p, size) && on_device(x, device);
+}
+
+static int optional_vector(PyObject *x, int64_t need, int64_t *device, void **p) {
+    *p = NULL;
+    return x == Py_None || vector_of(x, t_float[0], need, device, p);
+}
+
+/* lookup(cc_embedding_lookup, table, ids, out, scale, p, seed, site, first_row, stream) */
+static PyObject *m_lookup(PyObject *self, PyObject *const *a, Py_ssize_t n_args) {
+    (void)self;
+    void *fn, *ids, *stream;
+    Matrix table, out;
+    Drop d;
+    double scale;
+    int32_t id_bytes;
+    int64_t n, device = -1;
+    if (n_args != 10 || !address(a[0], &fn) || !matrix_of(a[1], 0, &device, &table) ||
+        !ids_of(a[2], &device, &ids, &id_bytes, &n) || !matrix_of(a[3], 0, &device, &out) ||
+        out.rows != n || out.cols != table.cols || (out.code != table.code && table.code != 0) ||
+        !real(a[4], &scale) || !drop_of(a + 5, &d) || !device_stream(a[9], device, &stream))
+        return no_call();
+    CALL(((lookup_fn)fn)(table.p, table.rows, table.stride, table.code, ids, id_bytes, n,
+                         (int32_t)table.cols, scale, d.p, d.seed, d.site, d.first_row, out.p,
+                         out.stride, out.code, stream));
+}
+
+/* grad(cc_embedding_grad, cc_embedding_grad_workspace_bytes, ids, grad_out, grad_table, workspace,
+ * scale, p, seed, site, first_row, accumulate, stream) */
+static PyObject *m_grad(PyObject *self, PyObject *const *a, Py_ssize_t n_args) {
+    (void)self;
+    void *fn, *size, *ids, *ws, *stream;
+    Matrix grad, table;
+    Drop d;
+    double scale;
+    int32_t id_bytes;
+    int64_t n, ws_bytes, device = -1;
+    if (n_args != 13 || !address(a[0], &fn) || !address(a[1], &size) ||
+        !ids_of(a[2], &device, &ids, &id_bytes, &n) || !matrix_of(a[3], 0, &device, &grad) ||
+        !matrix_of(a[4], 0, &device, &table) || grad.rows != n || grad.cols != table.cols ||
+        (table.code != grad.code && table.code != 0) || !real(a[6], &scale) || !drop_of(a + 7, &d) ||
+        (a[11] != Py_True && a[11] != Py_False) ||
+        !workspace_of(a[5], ((grad_bytes_fn)size)(n, table.rows, (int32_t)table.cols), &device, &ws,
+                      &ws_bytes) ||
+        !device_stream(a[12], device, &stream))
+        return no_call();
+    CALL(((grad_fn)fn)(ids, id_bytes, n, grad.p, grad.stride, grad.code, (int32_t)grad.cols, scale,
+                       d.p, d.seed, d.site, d.first_row, table.rows, table.p, table.stride,
+                       table.code, a[11] == Py_True, ws, ws_bytes, stream));
+}
+
+/* dropout(cc_dropout, x, out, p, seed, site, first_row, residual, stream) */
+static PyObject *m_dropout(PyObject *self, PyObject *const *a, Py_ssize_t n_args) {
+    (void)self;
+    void *fn, *stream;
+    Matrix x, out, res = {NULL, 0, 0, 0, 0};
+    Drop d;
+    int64_t device = -1;
+    if (n_args != 9 || !address(a[0], &fn) || !matrix_of(a[1], 0, &device, &x) ||
+        !matrix_of(a[2], 0, &device, &out) || out.rows != x.rows || out.cols != x.cols ||
+        out.code != x.code || !drop_of(a + 3, &d) ||
+        (a[7] != Py_None && (!matrix_of(a[7], 0, &device, &res) || res.rows != x.rows ||
+                             res.cols != x.cols || res.code != x.code)) ||
+        !device_stream(a[8], device, &stream))
+        return no_call();
+    CALL(((dropout_fn)fn)(x.p, x.stride, res.p, res.stride, x.rows, (int32_t)x.cols, x.code, d.p,
+                          d.seed, d.site, d.first_row, out.p, out.stride, stream));
+}
+
+/* quantize(cc_quantize_rows, x, q, scales, stream) */
+static PyObject *m_quantize(PyObject *self, PyObject *const *a, Py_ssize_t n_args) {
+    (void)self;
+    void *fn, *scales, *stream;
+    Matrix x, q;
+    int64_t device = -1;
+    if (n_args != 5 || !address(a[0], &fn) || !matrix_of(a[1], 0, &device, &x) ||
+        !matrix_of(a[2], 1, &device, &q) || q.rows != x.rows || q.cols != (x.cols + 15) / 16 * 16 ||
+        !vector_of(a[3], t_float[0], x.rows, &device, &scales) ||
+        !device_stream(a[4], device, &stream))
+        return no_call();
+    CALL(((quantize_fn)fn)(x.p, x.stride, x.code, x.rows, (int32_t)x.cols, q.p, q.stride, scales,
+                           stream));
+}
+
+/* matmul(cc_matmul_i8, cc_matmul_i8_workspace_bytes, a, a_scales, b, b_scales, out, bias, relu,
+ * workspace, stream) */
+static PyObject *m_matmul(PyObject *self, PyObject *const *a, Py_ssize_t n_args) {
+    (void)self;
+    void *fn, *size, *sa, *sb, *bias, *ws, *stream;
+    Matrix x, w, out;
+    int64_t ws_bytes, device = -1;
+    if (n_args != 11 || !address(a[0], &fn) || !address(a[1], &size) ||
+        !matrix_of(a[2], 1, &device, &x) || !vector_of(a[3], t_float[0], x.rows, &device, &sa) ||
+        !matrix_of(a[4], 1, &device, &w) || w.cols != x.cols ||
+        !vector_of(a[5], t_float[0], w.rows, &device, &sb) || !matrix_of(a[6], 0, &device, &out) ||
+        out.rows != x.rows || out.cols != w.rows ||
+        !optional_vector(a[7], w.rows, &device, &bias) || (a[8] != Py_True && a[8] != Py_False) ||
+        !workspace_of(a[9], ((product_bytes_fn)size)(x.rows, w.rows, x.cols), &device, &ws,
+                      &ws_bytes) ||
+        !device_stream(a[10], device, &stream))
+        return no_call();
+    CALL(((matmul_fn)fn)(x.p, x.stride, sa, w.p, w.stride, sb, bias, x.rows, w.rows, x.cols,
+                         a[8] == Py_True, out.p, out.stride, out.code, ws, ws_bytes, stream));
+}
+
+/* linear(cc_linear_i8, cc_linear_i8_workspace_bytes, x, w, w_scales, out, bias, relu, workspace,
+ * stream) */
+static PyObject *m_linear(PyObject *self, PyObject *const *a, Py_ssize_t n_args) {
+    (void)self;
+    void *fn, *size, *sw, *bias, *ws, *stream;
+    Matrix x, w, out;
+    int64_t ws_bytes, device = -1;
+    if (n_args != 10 || !address(a[0], &fn) || !address(a[1], &size) ||
+        !matrix_of(a[2], 0, &device, &x) || !matrix_of(a[3], 1, &device, &w) ||
+        w.cols != (x.cols + 15) / 16 * 16 || !vector_of(a[4], t_float[0], w.rows, &device, &sw) ||
+        !matrix_of(a[5], 0, &device, &out) || out.rows != x.rows || out.cols != w.rows ||
+        out.code != x.code || !optional_vector(a[6], w.rows, &device, &bias) ||
+        (a[7] != Py_True && a[7] != Py_False) ||
+        !workspace_of(a[8], ((product_bytes_fn)size)(x.rows, w.rows, x.cols), &device, &ws,
+                      &ws_bytes) ||
+        !device_stream(a[9], device, &stream))
+        return no_call();
+    CALL(((linear_fn)fn)(x.p, x.stride, x.code, w.p, w.stride, sw, bias, x.rows, w.rows, x.cols,
+                         a[7] == Py_True, out.p, out.stride, ws, ws_bytes, stream));
+}
+
+/* init_layers(torch.float32, torch.float16, torch.bfloat16, torch.int32, get_device, raw_stream) */
+static PyObject *m_init_layers(PyObject *self, PyObject *args) {
+    (void)self;
+    PyObject *o[6];
+    if (!PyArg_ParseTuple(args, "OOOOOO", o, o + 1, o + 2, o + 3, o + 4, o + 5))
+        return NULL;
+    PyObject **to[] = {t_float, t_float + 1, t_float + 2, &t_i32, &get_device, &raw_stream};
+    for (int i = 0; i < 6; ++i) {
+        Py_INCREF(o[i]);
+        Py_XSETREF(*to[i], o[i]);
+    }
+    Py_RETURN_NONE;
+}
+
 /* init(torch.Tensor, torch.int64, torch.int8, current_stream) */
 static PyObject *m_init(PyObject *self, PyObject *args) {
     (void)self;
@@ -351,6 +616,13 @@ static PyMethodDef methods[] = {
     {"resolve", (PyCFunction)(void (*)(void))m_resolve, METH_FASTCALL, "cc_resolve_ids"},
     {"upsert", (PyCFunction)(void (*)(void))m_upsert, METH_FASTCALL, "cc_store_upsert"},
     {"sort", (PyCFunction)(void (*)(void))m_sort, METH_FASTCALL, "cc_sort_affinity_method"},
+    {"init_layers", m_init_layers, METH_VARARGS, "The types and queries that the functions below need too."},
+    {"lookup", (PyCFunction)(void (*)(void))m_lookup, METH_FASTCALL, "cc_embedding_lookup"},
+    {"grad", (PyCFunction)(void (*)(void))m_grad, METH_FASTCALL, "cc_embedding_grad"},
+    {"dropout", (PyCFunction)(void (*)(void))m_dropout, METH_FASTCALL, "cc_dropout"},
+    {"quantize", (PyCFunction)(void (*)(void))m_quantize, METH_FASTCALL, "cc_quantize_rows"},
+    {"matmul", (PyCFunction)(void (*)(void))m_matmul, METH_FASTCALL, "cc_matmul_i8"},
+    {"linear", (PyCFunction)(void (*)(void))m_linear, METH_FASTCALL, "cc_linear_i8"},
     {NULL, NULL, 0, NULL}};
 
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal",
@@ -367,7 +639,8 @@ PyMODINIT_FUNC PyInit__marshal(void) {
     n_stride = PyUnicode_InternFromString("stride");
     n_element_size = PyUnicode_InternFromString("element_size");
     n_cuda_stream = PyUnicode_InternFromString("cuda_stream");
-    if (!n_cuda_stream || !n_dtype || !n_is_cuda || !n_numel || !n_contiguous || !n_data_ptr || !n_shape ||
+    n_get_device = PyUnicode_InternFromString("get_device");
+    if (!n_cuda_stream || !n_get_device || !n_dtype || !n_is_cuda || !n_numel || !n_contiguous || !n_data_ptr || !n_shape ||
         !n_stride || !n_element_size)
         return NULL;
     return PyModule_Create(&module);

@@ -53,6 +53,17 @@ class _Layers:
             f.argtypes = args
             f.restype = i64 if name.endswith("_bytes") else st
             setattr(self, name, f)
+        # Native marshalling (csrc/marshal.c) of plain calls: None from it means that the checks below
+        # decide. It takes function addresses.
+        try:
+            raw, device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+            L.marshal.init_layers(torch.float32, torch.float16, torch.bfloat16, torch.int32, device,
+                                  raw)
+            self.marshal = L.marshal
+        except AttributeError:
+            self.marshal = _b._ChecksOnly()
+        for name in sig:
+            setattr(self, "at_" + name, ctypes.cast(getattr(L, name), vp).value)
         self.codes = {torch.float32: CC_F32, torch.float16: CC_F16, torch.bfloat16: CC_BF16}
         self.id_bytes = {torch.int64: 8, torch.int32: 4}
         self.i8, self.f32 = torch.int8, torch.float32
@@ -140,7 +151,11 @@ def cc_embedding_lookup(table, ids, out, scale: float = 1.0, p: float = 0.0, see
                         site: int = 0, first_row: int = 0, stream=None) -> None:
     """out[t] = table[ids[t]] * scale with dropout of probability p; an id outside the table gives
     a zero row (see include/cc_layers.h)."""
-    L = _load()
+    L = _layers or _load()
+    st = L.marshal.lookup(L.at_cc_embedding_lookup, table, ids, out, scale, p, seed, site,
+                          first_row, stream)
+    if st is not None:
+        return _check(st, "cc_embedding_lookup")
     pt, table_stride, rows, cols = _matrix(table, "table")
     pi, id_bytes, n = _ids(L, ids)
     po, out_stride, out_rows, _ = _matrix(out, "out", cols)
@@ -164,7 +179,11 @@ def cc_embedding_grad(ids, grad_out, grad_table, workspace, scale: float = 1.0, 
                       stream=None) -> None:
     """grad_table[r] = the sum of grad_out's rows whose id is r, with the scale and the dropout mask
     of the lookup; with `accumulate` added to what grad_table holds. Equal calls give equal bits."""
-    L = _load()
+    L = _layers or _load()
+    st = L.marshal.grad(L.at_cc_embedding_grad, L.at_cc_embedding_grad_workspace_bytes, ids, grad_out,
+                        grad_table, workspace, scale, p, seed, site, first_row, accumulate, stream)
+    if st is not None:
+        return _check(st, "cc_embedding_grad")
     pi, id_bytes, n = _ids(L, ids)
     pt, table_stride, rows, cols = _matrix(grad_table, "grad_table")
     pg, grad_stride, grad_rows, _ = _matrix(grad_out, "grad_out", cols)
@@ -186,7 +205,10 @@ def cc_dropout(x, out, p: float, seed: int, site: int = 0, first_row: int = 0, r
                stream=None) -> None:
     """out = dropout(x) (+ residual): the mask is drawn from (seed, site, first_row + row, column),
     so the same call on a gradient is the backward pass. out may be x or residual."""
-    L = _load()
+    L = _layers or _load()
+    st = L.marshal.dropout(L.at_cc_dropout, x, out, p, seed, site, first_row, residual, stream)
+    if st is not None:
+        return _check(st, "cc_dropout")
     px, x_stride, n, cols = _matrix(x, "x")
     po, out_stride, out_rows, _ = _matrix(out, "out", cols)
     if out_rows != n:
@@ -214,7 +236,10 @@ def _padded(k: int) -> int:
 def cc_quantize_rows(x, q, scales, stream=None) -> None:
     """q, scales: the rows of x in 8-bit integers and one factor per row. q has x's columns rounded
     up to a multiple of 16, the added ones zero."""
-    L = _load()
+    L = _layers or _load()
+    st = L.marshal.quantize(L.at_cc_quantize_rows, x, q, scales, stream)
+    if st is not None:
+        return _check(st, "cc_quantize_rows")
     px, x_stride, n, cols = _matrix(x, "x")
     if q.dtype != L.i8:
         _fail("q", f"must be int8 (is {q.dtype})", TypeError)
@@ -245,7 +270,11 @@ def cc_matmul_i8(a, a_scales, b, b_scales, out, bias=None, relu: bool = False, w
                  stream=None) -> None:
     """out = act(a b' * a_scales * b_scales + bias) for int8 a [m, k] and b [n, k], k a multiple of
     16; the integer sums are exact."""
-    L = _load()
+    L = _layers or _load()
+    st = L.marshal.matmul(L.at_cc_matmul_i8, L.at_cc_matmul_i8_workspace_bytes, a, a_scales, b,
+                          b_scales, out, bias, relu, workspace, stream)
+    if st is not None:
+        return _check(st, "cc_matmul_i8")
     if a.dtype != L.i8:
         _fail("a", f"must be int8 (is {a.dtype})", TypeError)
     pa, a_stride, m, k = _matrix(a, "a")
@@ -269,7 +298,11 @@ def cc_linear_i8(x, w, w_scales, out, bias=None, relu: bool = False, workspace=N
                  stream=None) -> None:
     """out = act(x W' + bias) with x quantised row by row in the call and weights that
     cc_quantize_rows has put in 8 bits: w [n, columns of x rounded up to a multiple of 16]."""
-    L = _load()
+    L = _layers or _load()
+    st = L.marshal.linear(L.at_cc_linear_i8, L.at_cc_linear_i8_workspace_bytes, x, w, w_scales, out,
+                          bias, relu, workspace, stream)
+    if st is not None:
+        return _check(st, "cc_linear_i8")
     px, x_stride, m, k = _matrix(x, "x")
     t = _type(L, x, "x")
     pw, w_stride, n, pws, pbias = _weights(L, w, w_scales, bias, "w", _padded(k))

@@ -167,8 +167,10 @@ class Stub:
         self.calls = []
         for k in ("codes", "id_bytes", "i8", "f32"):
             setattr(self, k, getattr(real, k))
+        self.marshal = B._ChecksOnly()
         self.current_device = lambda: 0
         for name in Y.EXPORTS:
+            setattr(self, "at_" + name, 0)
             if name.endswith("_bytes"):
                 setattr(self, name, getattr(real, name))
             else:
@@ -192,7 +194,7 @@ class At(OnGpu):
 @pytest.fixture
 def stub(monkeypatch):
     s = Stub()
-    monkeypatch.setattr(Y, "_load", lambda: s)
+    monkeypatch.setattr(Y, "_layers", s)
     return s
 
 
@@ -308,6 +310,14 @@ def test_binding_refuses_another_current_device(stub):
     with pytest.raises(ValueError, match="current device"):
         Y.cc_dropout(g(4, 8), g(4, 8), 0.5, 1, stream=0)
     assert stub.calls == []
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_native_marshalling_leaves_host_tensors_to_the_checks(name):
+    """Host tensors are not plain: the native function answers None, and the checks word the error."""
+    a = {k: v.t if isinstance(v, OnGpu) else v for k, v in CALLS[name]().items()}
+    with pytest.raises(ValueError, match="GPU memory"):
+        getattr(Y, name)(**a, stream=0)
 
 
 def test_status_raises(stub):

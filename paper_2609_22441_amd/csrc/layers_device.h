@@ -61,17 +61,32 @@ struct Raw {
     }
 };
 
-// Lanes 4 i to 4 i + 3 that hold consecutive blocks of 32 bits move them between each other, so that
-// every access of a wavefront covers whole 64-byte pieces of memory where its own blocks would be
-// every second 16 bytes of it: such halves read and write 5.0 TB/s, whole pieces 6.5.
-template <int A, int B, int C, int D>
+// A block of 32-bit elements is two 16-byte pieces, so a wavefront's own blocks would be every second
+// piece of memory: half cache lines, which past the caches move at 3 TB/s where whole ones reach 6.5.
+// Lanes that hold consecutive blocks of one row therefore exchange pieces, and each access of four of
+// them covers 64 bytes, of eight 128: the lane with number q of its 4 or 8 moves piece q of theirs,
+// then piece q + 4 or q + 8.
+enum : int { kAlone = 0, kFour = 4, kEight = 8 };
+
+// How many lanes may exchange pieces, where lanes of consecutive numbers hold consecutive blocks and
+// lane 0 a multiple of 8 of them: those whose blocks are all full.
+__device__ __forceinline__ int exchange_of(uint32_t block, int cols) {
+    return (int)((block | 7) + 1) * kCols <= cols   ? kEight
+           : (int)((block | 3) + 1) * kCols <= cols ? kFour
+                                                    : kAlone;
+}
+
+template <int CONTROL>
 __device__ __forceinline__ words_t of_lanes(words_t x) {
     words_t y;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        y[i] = __builtin_amdgcn_mov_dpp((int)x[i], A | B << 2 | C << 4 | D << 6, 0xf, 0xf, true);
+        y[i] = __builtin_amdgcn_mov_dpp((int)x[i], CONTROL, 0xf, 0xf, true);
     return y;
 }
+
+constexpr int quad_perm(int a, int b, int c, int d) { return a | b << 2 | c << 4 | d << 6; }
+constexpr int kRowLeft4 = 0x104, kRowRight4 = 0x114;      // from the lane 4 further, 4 before
 
 __device__ __forceinline__ words_t either(bool c, words_t x, words_t y) {
     words_t z;
@@ -81,10 +96,29 @@ __device__ __forceinline__ words_t either(bool c, words_t x, words_t y) {
     return z;
 }
 
-// Whether that holds for a lane with this block, where lanes of consecutive numbers hold consecutive
-// blocks and 0 goes with 0: its four lanes' blocks are full.
-__device__ __forceinline__ bool quad_of(uint32_t block, int cols) {
-    return (int)((block | 3) + 1) * kCols <= cols;
+// Of four lanes' blocks (a, b), the pieces q and q + 4; back again.
+__device__ __forceinline__ void to_pieces4(words_t &a, words_t &b) {
+    const bool odd = threadIdx.x & 1;
+    const words_t lower = either(odd, of_lanes<quad_perm(0, 0, 1, 1)>(b),
+                                 of_lanes<quad_perm(0, 0, 1, 1)>(a));
+    b = either(odd, of_lanes<quad_perm(2, 2, 3, 3)>(b), of_lanes<quad_perm(2, 2, 3, 3)>(a));
+    a = lower;
+}
+
+__device__ __forceinline__ void from_pieces4(words_t &a, words_t &b) {
+    const bool upper = threadIdx.x & 2;
+    const words_t first = either(upper, of_lanes<quad_perm(0, 2, 0, 2)>(b),
+                                 of_lanes<quad_perm(0, 2, 0, 2)>(a));
+    b = either(upper, of_lanes<quad_perm(1, 3, 1, 3)>(b), of_lanes<quad_perm(1, 3, 1, 3)>(a));
+    a = first;
+}
+
+// Between the pieces q and q + 4 of the fours and q and q + 8 of their eight: its own inverse.
+__device__ __forceinline__ void swap_fours(words_t &a, words_t &b) {
+    const bool second = threadIdx.x & 4;
+    const words_t c = either(second, of_lanes<kRowRight4>(b), a);
+    b = either(second, b, of_lanes<kRowLeft4>(a));
+    a = c;
 }
 
 template <typename T>
@@ -105,23 +139,18 @@ __device__ __forceinline__ Raw<T> load_once(const T *p) {
     return r;
 }
 
-// Where a load of a block of 32 bits takes its two words from; settle() then puts them in place.
-struct Pieces {
-    int first, second;
-    __device__ explicit Pieces(bool quad)
-        : first(quad ? -(int)(threadIdx.x & 3) : 0), second(quad ? first + 4 : first + 1) {}
-};
-
+// The load of a block whose lane exchanges pieces; settle() puts them in place.
 template <bool ONCE, typename T>
-__device__ __forceinline__ Raw<T> load_pieces(const T *p, bool quad) {
+__device__ __forceinline__ Raw<T> load_pieces(const T *p, int exchange) {
     Raw<T> r;
     const words_t *w = (const words_t *)p;
     if constexpr (Raw<T>::kWords == 2) {
-        const Pieces at(quad);
+        w -= threadIdx.x & (exchange ? exchange - 1 : 0);
+        const words_t *second = w + (exchange ? exchange : 1);
         // Non-temporal: what is read once leaves the caches to what is read again, and comes at
         // 6.7 TB/s where other loads reach 5.9 (rows of 4 KiB in any order).
-        r.w[0] = ONCE ? __builtin_nontemporal_load(w + at.first) : w[at.first];
-        r.w[1] = ONCE ? __builtin_nontemporal_load(w + at.second) : w[at.second];
+        r.w[0] = ONCE ? __builtin_nontemporal_load(w) : *w;
+        r.w[1] = ONCE ? __builtin_nontemporal_load(second) : *second;
     } else {
         r.w[0] = ONCE ? __builtin_nontemporal_load(w) : *w;
     }
@@ -129,13 +158,15 @@ __device__ __forceinline__ Raw<T> load_pieces(const T *p, bool quad) {
 }
 
 template <typename T>
-__device__ __forceinline__ void settle(Raw<T> &r, bool quad) {
+__device__ __forceinline__ void settle(Raw<T> &r, int exchange) {
     if constexpr (Raw<T>::kWords == 2) {
-        const bool upper = threadIdx.x & 2;
-        const words_t a = either(upper, of_lanes<0, 2, 0, 2>(r.w[1]), of_lanes<0, 2, 0, 2>(r.w[0]));
-        const words_t b = either(upper, of_lanes<1, 3, 1, 3>(r.w[1]), of_lanes<1, 3, 1, 3>(r.w[0]));
-        r.w[0] = either(quad, a, r.w[0]);
-        r.w[1] = either(quad, b, r.w[1]);
+        words_t a = r.w[0], b = r.w[1];
+        swap_fours(a, b);
+        a = either(exchange == kEight, a, r.w[0]);
+        b = either(exchange == kEight, b, r.w[1]);
+        from_pieces4(a, b);
+        r.w[0] = either(exchange != kAlone, a, r.w[0]);
+        r.w[1] = either(exchange != kAlone, b, r.w[1]);
     }
 }
 
@@ -174,27 +205,23 @@ __device__ __forceinline__ void store_block(T *p, const float (&x)[kCols]) {
 }
 
 // The same as store_block past the caches' reach, for outputs that would push out of the caches what
-// the kernel reads more than once. `quad`: the lane's four lanes are all here, with the full blocks
-// that follow each other in one row.
+// the kernel reads more than once. The lanes that exchange pieces are all here.
 template <typename T>
-__device__ __forceinline__ void stream_block(T *p, const float (&x)[kCols], bool quad) {
+__device__ __forceinline__ void stream_block(T *p, const float (&x)[kCols], int exchange) {
     const Raw<T> r = packed<T>(x);
     if constexpr (Raw<T>::kWords == 2) {
-        const bool odd = threadIdx.x & 1;
-        const words_t lower = either(odd, of_lanes<0, 0, 1, 1>(r.w[1]), of_lanes<0, 0, 1, 1>(r.w[0]));
-        const words_t upper = either(odd, of_lanes<2, 2, 3, 3>(r.w[1]), of_lanes<2, 2, 3, 3>(r.w[0]));
-        if (quad) {
-            // Of the eight pieces of the four blocks this lane stores the one of its own number, then
-            // the one four further.
-            words_t *first = (words_t *)p - (threadIdx.x & 3);
-            __builtin_nontemporal_store(lower, first);
-            __builtin_nontemporal_store(upper, first + 4);
-            return;
-        }
+        words_t a = r.w[0], b = r.w[1];
+        to_pieces4(a, b);
+        words_t c = a, d = b;
+        swap_fours(c, d);
+        a = exchange == kEight ? c : exchange == kFour ? a : r.w[0];
+        b = exchange == kEight ? d : exchange == kFour ? b : r.w[1];
+        words_t *w = (words_t *)p - (threadIdx.x & (exchange ? exchange - 1 : 0));
+        __builtin_nontemporal_store(a, w);
+        __builtin_nontemporal_store(b, w + (exchange ? exchange : 1));
+    } else {
+        __builtin_nontemporal_store(r.w[0], (words_t *)p);
     }
-#pragma unroll
-    for (int i = 0; i < Raw<T>::kWords; ++i)
-        __builtin_nontemporal_store(r.w[i], (words_t *)p + i);
 }
 
 template <typename T>
@@ -208,17 +235,17 @@ __device__ __forceinline__ void store_block(T *p, const float (&x)[kCols], int c
 // A block of the row at p. TAIL: rows have a last block of fewer columns, or are not aligned to 16
 // bytes (then accesses share cache lines, and what bypasses the caches moves them twice); its lanes read the block
 // before it first (in rows of one block nothing), so that the loads of all lanes are in flight before
-// the first of them is waited for. `quad` as for stream_block.
+// the first of them is waited for.
 template <bool TAIL, bool ONCE, typename T>
-__device__ __forceinline__ Raw<T> load_most(const T *p, int col, int cols, bool quad) {
+__device__ __forceinline__ Raw<T> load_most(const T *p, int col, int cols, int exchange) {
     if (TAIL && cols < kCols)
         return Raw<T>{};
-    return load_pieces<ONCE && !TAIL>(p + (TAIL && col + kCols > cols ? col - kCols : col), quad);
+    return load_pieces<ONCE && !TAIL>(p + (TAIL && col + kCols > cols ? col - kCols : col), exchange);
 }
 
 template <bool TAIL, typename T>
-__device__ __forceinline__ void load_rest(Raw<T> &x, const T *p, int col, int cols, bool quad) {
-    settle(x, quad);
+__device__ __forceinline__ void load_rest(Raw<T> &x, const T *p, int col, int cols, int exchange) {
+    settle(x, exchange);
     if (TAIL && col + kCols > cols)
         x = load_block(p + col, cols - col);
 }

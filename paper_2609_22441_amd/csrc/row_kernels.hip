@@ -73,19 +73,19 @@ __global__ __launch_bounds__(kRowThreads) void row_kernel(RowLaunch l) {
         }
         Raw<TI> x[U];
         Raw<TO> res[U];
-        bool quad[U];
+        int exchange[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int col = block[u] * kCols;
-            // Four lanes are in one row where its blocks are a multiple of four, and then all here:
-            // a tile starts at a multiple of four as well.
-            quad[u] = !(l.blocks & 3) && quad_of(block[u], a.cols);
+            // Lanes 4 or 8 i on are in one row where its blocks are a multiple of 4 or 8, and then all
+            // here: a tile starts at a multiple of 8 blocks as well.
+            exchange[u] = TAIL || l.blocks % 4 ? kAlone : l.blocks % 8 ? kFour : kEight;
             x[u] = load_most<TAIL, !kIds>((const TI *)((const char *)a.src + src[u] * a.src_stride), col,
-                                   a.cols, quad[u]);
+                                   a.cols, exchange[u]);
             if (RES)
                 res[u] = load_most<TAIL, true>(
                     (const TO *)((const char *)a.res + min(row[u], a.n - 1) * a.res_stride), col,
-                    a.cols, quad[u]);
+                    a.cols, exchange[u]);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -93,10 +93,10 @@ __global__ __launch_bounds__(kRowThreads) void row_kernel(RowLaunch l) {
                 continue;
             const int col = block[u] * kCols;
             load_rest<TAIL>(x[u], (const TI *)((const char *)a.src + src[u] * a.src_stride), col,
-                            a.cols, quad[u]);
+                            a.cols, exchange[u]);
             if (RES)
                 load_rest<TAIL>(res[u], (const TO *)((const char *)a.res + row[u] * a.res_stride),
-                                col, a.cols, quad[u]);
+                                col, a.cols, exchange[u]);
             float y[kCols];
             row_values<DROP, RES>(a, x[u], res[u], row[u], block[u], found[u], y);
             TO *p = (TO *)((char *)a.out + row[u] * a.out_stride) + col;
@@ -105,7 +105,7 @@ __global__ __launch_bounds__(kRowThreads) void row_kernel(RowLaunch l) {
             else if (TAIL)
                 store_block(p, y);
             else
-                stream_block(p, y, quad[u]);
+                stream_block(p, y, exchange[u]);
         }
     }
 }
@@ -126,7 +126,7 @@ __global__ __launch_bounds__(kRowThreads) void wide_kernel(RowLaunch l) {
         if (row0 >= a.n || block >= (uint32_t)l.blocks)
             continue;
         const int col = block * kCols;
-        const bool quad = quad_of(block, a.cols);
+        const int exchange = exchange_of(block, a.cols);
         int64_t src[U];
         const TI *from[U];
         bool found[U];
@@ -145,21 +145,21 @@ __global__ __launch_bounds__(kRowThreads) void wide_kernel(RowLaunch l) {
         Raw<TO> res[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            x[u] = load_most<TAIL, !kIds>(from[u], col, a.cols, quad);
+            x[u] = load_most<TAIL, !kIds>(from[u], col, a.cols, exchange);
             if (RES)
                 res[u] = load_most<TAIL, true>(
                     (const TO *)((const char *)a.res + min(row0 + u, a.n - 1) * a.res_stride), col,
-                    a.cols, quad);
+                    a.cols, exchange);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t row = row0 + u;
             if (row >= a.n)
                 break;
-            load_rest<TAIL>(x[u], from[u], col, a.cols, quad);
+            load_rest<TAIL>(x[u], from[u], col, a.cols, exchange);
             if (RES)
                 load_rest<TAIL>(res[u], (const TO *)((const char *)a.res + row * a.res_stride), col,
-                                a.cols, quad);
+                                a.cols, exchange);
             float y[kCols];
             row_values<DROP, RES>(a, x[u], res[u], row, block, found[u], y);
             TO *p = (TO *)((char *)a.out + row * a.out_stride) + col;
@@ -168,7 +168,7 @@ __global__ __launch_bounds__(kRowThreads) void wide_kernel(RowLaunch l) {
             else if (TAIL)
                 store_block(p, y);
             else
-                stream_block(p, y, quad);
+                stream_block(p, y, exchange);
         }
     }
 }

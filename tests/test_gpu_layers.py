@@ -148,7 +148,9 @@ def skewed(r, n, rows, kind):
 @pytest.mark.parametrize("n,rows,cols", [(1, 1, 5), (1, 700, 40), (2, 2, 16), (64, 3, 33),
                                          (65, 511, 8), (2_049, 512, 24), (4_096, 1, 16),
                                          (4_097, 1_000, 100), (9_000, 70_000, 16),
-                                         (20_000, 51, 3), (5_000, 300_000, 2)])
+                                         (20_000, 51, 3), (5_000, 300_000, 2), (4_096, 64, 520),
+                                         (3_000, 17, 1_100), (4_097, 130, 1_030),
+                                         (150_000, 40, 16), (300_000, 9_000, 8)])
 def test_grad_of_skewed_ids(kind, n, rows, cols):
     """Runs that cross many chunks, tables far larger and far smaller than the call, one to three
     digits, and rows that no id points at."""
@@ -190,6 +192,10 @@ def test_grad_of_nothing():
     got = run_grad(none, torch.empty(0, 40), 70, 40, "f32", accumulate=before)
     assert (got == before.double().numpy()).all()
     ws = torch.empty(0, dtype=torch.uint8, device=DEV)
+    P.cc_embedding_grad(torch.empty(0, dtype=torch.int64, device=DEV), torch.empty(0, 8, device=DEV),
+                        torch.empty(70_000, 8, device=DEV),
+                        torch.empty(P.cc_embedding_grad_workspace_bytes(0, 70_000, 8),
+                                    dtype=torch.uint8, device=DEV))
     P.cc_embedding_grad(torch.zeros(3, dtype=torch.int64, device=DEV), torch.zeros(3, 8, device=DEV),
                         torch.empty(0, 8, device=DEV), ws)
 

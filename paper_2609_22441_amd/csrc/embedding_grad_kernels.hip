@@ -7,15 +7,16 @@
 //
 //   sum    the sorted tokens are cut into chunks of equal length, whatever the ids are, so that an
 //          id that takes most of the tokens is shared out as evenly as ids that occur once. A group
-//          of lanes adds a chunk's rows in 32 bits, run by run; a run that lies inside the chunk is
-//          finished and written, one that crosses an edge of it is kept as a partial sum. Further
-//          workgroups of the same launch write zeros into the rows that no id points at.
+//          of lanes adds a chunk's rows in 32 bits, run by run, and writes each run's sum; a run that
+//          ends inside the next chunk is added up to its end, and that chunk begins after it. Only of
+//          a run that covers whole chunks does each of them keep a partial sum. Further workgroups of
+//          the same launch write zeros into the rows that no id points at.
 //   fold   the same once more, with the partial sums of kFold chunks in the tokens' place: an id with
-//          tens of thousands of tokens leaves hundreds of them. Left out where few are possible.
-//   join   what crosses edges still is added up, one workgroup a run, in the order of the chunks.
+//          all of a million tokens leaves tens of thousands of them. Left out where few are possible.
+//   join   the partial sums of each run are added up by a workgroup, in the order of the chunks.
 //
-// The work is bound by the bytes of grad_out and grad_table: pairs are 8 bytes a token, partial
-// sums at most 8 bytes a column of every chunk.
+// The work is bound by the bytes of grad_out and grad_table: pairs are 8 bytes a token, and the partial
+// sums are 4 bytes a column of chunks that one id covers.
 #include <algorithm>
 
 #include "layers_device.h"
@@ -76,12 +77,15 @@ struct FromPairs {
 };
 
 // Counts of each digit value in every tile: counts[tile][digit]. The first pass's launch has further
-// workgroups that clear `found`, a byte for every row of the table.
+// workgroups that clear `found`, a byte for every row of the table, and empties the list of runs.
 template <typename Source>
 __global__ __launch_bounds__(kSortThreads) void digit_counts(Source source, int64_t n, int64_t tile,
                                                              int shift, int digits, int tiles,
                                                              uint32_t *counts, words_t *found,
-                                                             int64_t found_words) {
+                                                             int64_t found_words,
+                                                             uint32_t *list_count) {
+    if (list_count && blockIdx.x == 0 && threadIdx.x == 0)
+        *list_count = 0;
     if ((int)blockIdx.x >= tiles) {
         const int64_t first = (int64_t)((int)blockIdx.x - tiles) * kClearWords;
         const int64_t last = min(found_words, first + kClearWords);
@@ -215,12 +219,34 @@ struct Runs {
     int32_t width;               // floats per partial row, a multiple of 8
     int32_t blocks;              // column blocks per row
     int32_t tiles;               // of 64 blocks or fewer each
+    int64_t whole;               // tokens of the chunks that the partial sums come from
+    bool listed;                 // the sums list their runs (no fold after them)
+    uint32_t *list;              // [0]: how many; then the chunks in which runs start that the join adds up
+    // By the one lane of a chunk that speaks for it. The order of the list changes no result.
+    __device__ void append(int64_t c) const { list[1 + atomicAdd(list, 1u)] = (uint32_t)c; }
+    // How many of the `chunk` pairs from i on have the key, by all lanes of a wavefront, L of them for
+    // one i: the pairs are sorted, and the first does or none.
+    template <int L>
+    __device__ int leading(int64_t i, uint32_t key) const {
+        const int lane = threadIdx.x & 63, in = lane % L;
+        int count = 0;
+        for (int64_t j = in; j - in < chunk; j += L) {
+            const uint64_t same = __ballot(j < chunk && i + j < n && pairs[min(i + j, n - 1)].key == key);
+            count += __popcll(L == 64 ? same : same >> (lane - in) & (((uint64_t)1 << L % 64) - 1));
+        }
+        return count;
+    }
+    // Whether a run that has the pair before i1 goes on through the whole chunk from i1 on.
+    __device__ bool goes_on(int64_t i1, uint32_t key) const {
+        return i1 < n && pairs[i1].key == key && pairs[min(n, i1 + whole) - 1].key == key;
+    }
     __device__ int64_t chunk_of(int64_t group) const {
         return tiles == 1 ? group : (int64_t)((uint32_t)group / (uint32_t)tiles);
     }
 };
 
 constexpr int kJoinThreads = 1024;
+constexpr int64_t kJoinGrid = 512;      // two workgroups per unit
 constexpr int kFold = 16;        // chunks whose partial sums are added up together
 
 // A group's pairs: through the scalar cache where the group is a wavefront.
@@ -290,15 +316,21 @@ __global__ __launch_bounds__(256) void sum_kernel(GradArgs a, Runs r, uint32_t s
                                    : threadIdx.x / L);
     const int64_t c = r.chunk_of(group);
     const int block = (int)(group - c * r.tiles) * L + (int)(threadIdx.x % L);
+    const auto pairs = pairs_of<L>(r.pairs);
+    const int64_t start = min(c, r.chunks - 1) * r.chunk, stop = min(r.n, start + r.chunk);
+    const uint32_t low = pairs[start].key, high = pairs[stop - 1].key;
+    const int of_low = r.leading<L>(start, low), of_high = stop < r.n ? r.leading<L>(stop, high) : 0;
     if (c >= r.chunks || block >= r.blocks)
         return;
+    const bool began = start > 0 && pairs[start - 1].key == low;
+    const bool covers = of_low == stop - start, next = of_high == min(r.chunk, r.n - stop);
+    // The chunk's own tokens; whether its first run began before it, and its last goes on past it.
+    const int64_t i0 = start + (began && !covers ? of_low : 0);
+    const int64_t i1 = stop + (next ? 0 : of_high);
+    const bool head = began && covers, tail = of_high && next;
     const int col = block * kCols;
     const int exchange = exchange_of(block, a.cols);
-    const auto pairs = pairs_of<L>(r.pairs);
-    const int64_t i0 = c * r.chunk, i1 = min(r.n, i0 + r.chunk);
     uint32_t current = pairs[i0].key;
-    const bool head = i0 > 0 && pairs[i0 - 1].key == current;
-    const bool tail = i1 < r.n && pairs[i1].key == pairs[i1 - 1].key;
     bool first = true;
     float sum[kCols] = {};
     auto finish = [&](bool open) {
@@ -328,16 +360,16 @@ __global__ __launch_bounds__(256) void sum_kernel(GradArgs a, Runs r, uint32_t s
             sum[k] += !DROP || bits.kept(k, a.mask.threshold) ? v : 0.0f;
         }
     };
-    // kAhead rows are added while the next kAhead are on their way; the last chunk's odd ones one by
-    // one. Ids outside the table come last and end the loop.
+    // kAhead rows are added while the next kAhead are on their way, then the rest. Ids outside the table
+    // come last and end the loop.
     constexpr int kAhead = 4;
     uint32_t key[2][kAhead], token[2][kAhead];
     Raw<TG> x[2][kAhead];
     auto fetch = [&](int s, int64_t i) {
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
-            key[s][j] = pairs[i + j].key;
-            token[s][j] = pairs[i + j].token;
+            key[s][j] = pairs[min(i + j, i1 - 1)].key;
+            token[s][j] = pairs[min(i + j, i1 - 1)].token;
         }
 #pragma unroll
         for (int j = 0; j < kAhead; ++j)
@@ -357,10 +389,19 @@ __global__ __launch_bounds__(256) void sum_kernel(GradArgs a, Runs r, uint32_t s
         for (int j = 0; j < kAhead; ++j)
             add(key[1][j], token[1][j], x[1][j]);
     }
-    for (int64_t i = even; i < i1 && pairs[i].key < (uint64_t)a.rows; ++i)
-        add(pairs[i].key, pairs[i].token,
-            load_most<TAIL, true>(grad_row<TG>(a, pairs[i].token), col, a.cols, exchange));
+    if (even < i1 && pairs[even].key < (uint64_t)a.rows) {
+        fetch(0, even);
+        if (even + kAhead < i1)
+            fetch(1, even + kAhead);
+#pragma unroll
+        for (int j = 0; j < 2 * kAhead; ++j)
+            if (even + j < i1)
+                add(key[j / kAhead][j % kAhead], token[j / kAhead][j % kAhead],
+                    x[j / kAhead][j % kAhead]);
+    }
     finish((first && head) || tail);
+    if (tail && !head && r.listed && block == 0 && current < (uint64_t)a.rows)
+        r.append(c);
 }
 
 // The partial sums of kFold chunks, a wavefront for 64 column blocks of them. A lane looks at one
@@ -379,10 +420,10 @@ __global__ __launch_bounds__(64) void fold_kernel(GradArgs a, Runs r, int tiles,
         const int64_t i0 = c * r.chunk, i1 = min(r.n, i0 + r.chunk);
         const uint32_t low = r.pairs[i0].key, high = r.pairs[i1 - 1].key;
         const bool head = i0 > 0 && r.pairs[i0 - 1].key == low;
-        goes_on = i1 < r.n && r.pairs[i1].key == high;
+        const bool inside = head && low == high;       // a run that began earlier covers the chunk
+        goes_on = r.goes_on(i1, high);
         key = lane & 1 ? high : low;
-        // One that is open at the chunk's start is kept there, though it may be at the end too.
-        held = lane & 1 ? goes_on && !(head && low == high) : head;
+        held = lane & 1 ? goes_on && !inside : inside;
         held &= key < (uint64_t)a.rows;
     }
     uint64_t places = __ballot(held);
@@ -422,6 +463,8 @@ __global__ __launch_bounds__(64) void fold_kernel(GradArgs a, Runs r, int tiles,
             if (next >= 0 && there == here)
                 continue;
             const bool leaves = next < 0 && last_open;
+            if (leaves && !open && block == 0)
+                r.append(f);
             if (live) {
                 if (open || leaves)
                     store_block(out + (f * 2 + (open ? 0 : 1)) * r.width + col, sum);
@@ -436,52 +479,73 @@ __global__ __launch_bounds__(64) void fold_kernel(GradArgs a, Runs r, int tiles,
     }
 }
 
-// A workgroup per chunk and tile of L column blocks: where a run starts in the chunk and goes on
-// past its end, adds up the run's partial sums. Lane groups take every (kJoinThreads / L)-th chunk of the
-// run, and the first adds their sums in order.
+// The sums of T / L lane groups, added up in their order into the first group's; by the whole workgroup.
+template <int L, int T>
+__device__ __forceinline__ void add_groups(float (&part)[T][kCols + 1]) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < L * kCols; i += T) {
+        float sum = part[i / kCols][i % kCols];
+#pragma unroll 8
+        for (int g = 1; g < T / L; ++g)
+            sum += part[g * L + i / kCols][i % kCols];
+        part[i / kCols][i % kCols] = sum;
+    }
+    __syncthreads();
+}
+
+// The runs that go on through whole chunks: for each and every tile of L column blocks a workgroup adds
+// up the partial sums. Lane groups take every (kJoinThreads / L)-th chunk of the run, and the first adds
+// their sums in order.
 template <typename TT, int L>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(GradArgs a, Runs r) {
     constexpr int kGroups = kJoinThreads / L;
-    const int64_t c = blockIdx.x / r.tiles;
-    const int64_t i0 = c * r.chunk, i1 = min(r.n, i0 + r.chunk);
-    const uint32_t key = r.pairs[i1 - 1].key;
-    const bool goes_on = i1 < r.n && r.pairs[i1].key == key && key < (uint64_t)a.rows;
-    const bool starts = i0 == 0 || r.pairs[i0].key != key || r.pairs[i0 - 1].key != key;
-    if (!goes_on || !starts)
-        return;
-    // The run's last chunk: a probe per thread and round of whether a chunk starts with the key.
-    int64_t end = c, past = r.chunks;                  // `end` does, or is c; `past` does not
-    while (past - end > 1) {
-        const int64_t step = (past - end + kJoinThreads - 1) / kJoinThreads;
-        const int64_t d = end + (threadIdx.x + 1) * step;
-        const int hits = __syncthreads_count(d < past && r.pairs[d * r.chunk].key == key);
-        end += hits * step;
-        past = min(past, end + step);
-    }
-    const int lane = threadIdx.x % L, group = threadIdx.x / L;
-    const int block = (int)(blockIdx.x - c * r.tiles) * L + lane;
-    const int col = block * kCols;
-    float sum[kCols] = {};
-    if (block < r.blocks)
-#pragma unroll 8
-        for (int64_t d = c + group; d <= end; d += kGroups) {
-            // The run is open at its first chunk's end and at the later ones' start.
-            const Raw<float> x = load_block(r.partial + (d * 2 + (d == c ? 1 : 0)) * r.width + col);
-#pragma unroll
-            for (int k = 0; k < kCols; ++k)
-                sum[k] += x[k];
-        }
     __shared__ float part[kJoinThreads][kCols + 1];
+    const uint32_t total = r.list[0] * (uint32_t)r.tiles;
+    for (uint32_t e = blockIdx.x; e < total; e += gridDim.x) {
+        const uint32_t entry = e / (uint32_t)r.tiles;
+        const int64_t c = r.list[1 + entry];
+        const uint32_t key = r.pairs[min(r.n, (c + 1) * r.chunk) - 1].key;
+        // The last chunk that holds a sum of the run: a probe per thread and round.
+        int64_t end = c, past = r.chunks;              // `end` does, or is c; `past` does not
+        while (past - end > 1) {
+            const int64_t step = (past - end + kJoinThreads - 1) / kJoinThreads;
+            const int64_t d = end + (threadIdx.x + 1) * step;
+            const int hits = __syncthreads_count(d < past && r.goes_on(d * r.chunk, key));
+            end += hits * step;
+            past = min(past, end + step);
+        }
+        const int lane = threadIdx.x % L, group = threadIdx.x / L;
+        const int block = (int)(e - entry * r.tiles) * L + lane;
+        const int col = block * kCols;
+        float sum[kCols] = {};
+        constexpr int kAhead = 8;                      // sums on their way
+        const float *from = r.partial + (block < r.blocks ? col : 0);
+        for (int64_t d = c + group; d <= end; d += kAhead * kGroups) {
+            Raw<float> x[kAhead];
 #pragma unroll
-    for (int k = 0; k < kCols; ++k)
-        part[threadIdx.x][k] = sum[k];
-    __syncthreads();
-    if (group == 0 && block < r.blocks) {
-        for (int g = 1; g < kGroups; ++g)
+            for (int j = 0; j < kAhead; ++j) {
+                // The run is open at its first chunk's end and at the later ones' start.
+                const int64_t at = min(d + j * kGroups, end);
+                x[j] = load_block(from + (at * 2 + (at == c ? 1 : 0)) * r.width);
+            }
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j)
+                if (d + j * kGroups <= end)
+#pragma unroll
+                    for (int k = 0; k < kCols; ++k)
+                        sum[k] += x[j][k];
+        }
+#pragma unroll
+        for (int k = 0; k < kCols; ++k)
+            part[threadIdx.x][k] = sum[k];
+        add_groups<L, kJoinThreads>(part);
+        if (group == 0 && block < r.blocks) {
 #pragma unroll
             for (int k = 0; k < kCols; ++k)
-                sum[k] += part[g * L + lane][k];
-        write_row<TT, true>(a, key, col, exchange_of(block, a.cols), sum);
+                sum[k] = part[lane][k];
+            write_row<TT, true>(a, key, col, exchange_of(block, a.cols), sum);
+        }
+        __syncthreads();
     }
 }
 
@@ -698,12 +762,11 @@ __global__ __launch_bounds__(256) void windows_kernel(GradArgs a, Window v) {
 #pragma unroll
     for (int k = 0; k < kCols; ++k)
         part[threadIdx.x][k] = sum[k];
-    __syncthreads();
+    add_groups<L, 256>(part);
     if (group == 0 && live) {
-        for (int g = 1; g < kGroups; ++g)
 #pragma unroll
-            for (int k = 0; k < kCols; ++k)
-                sum[k] += part[g * L + lane][k];
+        for (int k = 0; k < kCols; ++k)
+            sum[k] = part[lane][k];
         write_row<TT, true>(a, row, col, exchange_of(block, a.cols), sum);
     }
 }
@@ -718,7 +781,7 @@ struct Plan {
     int64_t chunk, chunks;
     int32_t lanes, tiles, width;
     int64_t folds;                                       // 0: none, the chunks are joined
-    int64_t counts, found, pairs0, pairs1, partial, folded, bytes;   // offsets, the total size
+    int64_t counts, found, list, pairs0, pairs1, partial, folded, bytes;  // offsets, the total size
 };
 
 Plan plan(int64_t n, int64_t rows, int32_t cols) {
@@ -753,9 +816,11 @@ Plan plan(int64_t n, int64_t rows, int32_t cols) {
         p.window.count = 1;
         return p;
     }
-    // Chunks of 64 tokens, in which the partial sums are at most 1/16 of 16-bit rows' bytes (1/32 of
-    // 32-bit ones'); shorter ones while the chip has fewer than 4 wavefronts per SIMD of them.
-    p.chunk = 32;
+    // Chunks of 16 tokens where rows are wide, so that the last wavefronts to run are few of many, and 32
+    // where more groups share a wavefront; shorter ones while the chip has fewer than 4 wavefronts per
+    // SIMD of them. 131,072 x 2,048 bf16, Zipf frequencies: 183 us in the sums with 16, 192 with 32, 207
+    // with 64.
+    p.chunk = p.lanes == 64 ? 16 : 32;
     while (p.chunk > 8 && n / p.chunk * p.tiles * p.lanes < 4 * 1024 * 64)
         p.chunk /= 2;
     while (n / p.chunk * p.tiles > kMaxChunks)
@@ -769,6 +834,7 @@ Plan plan(int64_t n, int64_t rows, int32_t cols) {
     };
     p.counts = take((int64_t)p.sort.tiles << p.sort.digit_bits << 2);
     p.found = take(rows + 1);               // the last: ids outside the table
+    p.list = take(4 * (p.chunks + 1));
     p.pairs0 = take(n * (int64_t)sizeof(Pair));
     p.pairs1 = take(p.sort.passes > 1 ? n * (int64_t)sizeof(Pair) : 0);
     p.partial = take(p.chunks * 2 * p.width * 4);
@@ -792,7 +858,7 @@ void launch_pass(Source source, const GradArgs &a, const Plan &p, int pass, Pair
     if (p.sort.tiles + clears > 0)
         digit_counts<<<(unsigned)(p.sort.tiles + clears), kSortThreads, 0, stream>>>(
             source, a.n, p.sort.tile, shift, 1 << p.sort.digit_bits, p.sort.tiles, counts,
-            (words_t *)found, words);
+            (words_t *)found, words, pass == 0 ? (uint32_t *)(ws + p.list) : nullptr);
     if (p.sort.tiles > 0)
         digit_scatter<<<p.sort.tiles, kSortThreads, 0, stream>>>(
             source, a.n, p.sort.tile, shift, p.sort.digit_bits, counts, p.sort.tiles, out, found);
@@ -839,7 +905,8 @@ void launch_sum(const GradArgs &a, const Runs &r, const Plan &p, hipStream_t str
         fold_kernel<TT><<<(unsigned)(p.folds * tiles), 64, 0, stream>>>(a, r, tiles, j.partial);
     }
     if (j.chunks > 1)
-        join_kernel<TT, L><<<(unsigned)(j.chunks * r.tiles), kJoinThreads, 0, stream>>>(a, j);
+        join_kernel<TT, L><<<(unsigned)std::min<int64_t>(j.chunks * r.tiles, kJoinGrid),
+                             kJoinThreads, 0, stream>>>(a, j);
 }
 
 template <typename TG, typename TT, int L>
@@ -886,7 +953,7 @@ hipError_t launch_embedding_grad(const GradArgs &a, hipStream_t stream) {
     }
     const Runs r{pairs[(p.sort.passes - 1) & 1], (const uint8_t *)(ws + p.found),
                  (float *)(ws + p.partial), a.n, p.chunk, p.chunks, p.width, blocks_of(a.cols),
-                 p.tiles};
+                 p.tiles, p.chunk, p.folds == 0, (uint32_t *)(ws + p.list)};
     if (a.grad_type == kF32)
         launch_lanes<float, float>(a, r, p, stream);
     else if (a.grad_type == kF16 && a.table_type == kF32)

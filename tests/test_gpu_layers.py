@@ -150,7 +150,8 @@ def skewed(r, n, rows, kind):
                                          (4_097, 1_000, 100), (9_000, 70_000, 16),
                                          (20_000, 51, 3), (5_000, 300_000, 2), (4_096, 64, 520),
                                          (3_000, 17, 1_100), (4_097, 130, 1_030),
-                                         (150_000, 40, 16), (300_000, 9_000, 8)])
+                                         (150_000, 40, 16), (300_000, 9_000, 8),
+                                         (20_000, 200, 136), (9_000, 129, 1_032)])
 def test_grad_of_skewed_ids(kind, n, rows, cols):
     """Runs that cross many chunks, tables far larger and far smaller than the call, one to three
     digits, and rows that no id points at."""

@@ -35,6 +35,10 @@ constexpr int64_t kSplitK = 1024;
 // Of products this short the output is the work.
 constexpr int64_t kShortK = 128, kShortTile = 128;
 
+// Of longer ones up to this a tile's loads and stores still cost as much as its products: two tiles at
+// a time on a unit, 50,000 x 2,048 x 512 117 / 133 in 256 x 256 (x 1,024 183 / 180).
+constexpr int64_t kMidK = 512;
+
 inline int64_t tiles_of(int64_t m, int64_t n, int64_t tm, int64_t tn) {
     return ((m + tm - 1) / tm) * ((n + tn - 1) / tn);
 }
@@ -55,6 +59,8 @@ inline int32_t product_choice(int64_t m, int64_t n, int64_t k) {
         return k >= kSplitK ? kTile128Split : kTile128;
     if (k <= kShortK)
         return kTileShort;
+    if (k <= kMidK)
+        return kTile128;
     // A unit has two 128 x 128 tiles at a time (87 for k = 8,192) or one of 256 x 256 (127): 1,024 x
     // 8,192 x 8,192 89 / 89, 2,048 x 8,192 x 8,192 127 in 256 x 256, 171 in 128 x 128.
     const int64_t r128 = (t128 + 2 * kUnits - 1) / (2 * kUnits), r256 = (t256 + kUnits - 1) / kUnits;

@@ -15,13 +15,14 @@ namespace {
 constexpr int kRowThreads = 256;
 constexpr int64_t kRowGrid = 1 << 20;             // workgroups at most; each then takes several tiles
 
-constexpr int kWideBlocks = 96;
+constexpr int kWideBlocks = 64;
 
 struct RowLaunch {
     RowArgs a;
     Divider div;
     int32_t blocks;                               // per row
     int32_t segments;                             // of 64 blocks, per row (wide rows)
+    bool by_segment;
     int64_t tiles;
 };
 
@@ -111,18 +112,23 @@ __global__ __launch_bounds__(kRowThreads) void row_kernel(RowLaunch l) {
 }
 
 // The same for rows of kWideBlocks blocks or more: a wavefront takes 64 blocks of U rows, so that
-// rows, ids and addresses are the wavefront's (scalar) and a lane keeps its columns. Workgroups go
-// round the segments of 64 blocks: with 8 of them each XCD's L2 holds one segment of the rows that
-// are looked up often, not all of fewer rows.
+// rows, ids and addresses are the wavefront's (scalar) and a lane keeps its columns. Four wavefronts
+// of a workgroup take segments that follow each other; where the rows are read in order and have a
+// multiple of 8 segments, rows that follow each other of one segment, so that each XCD reads and
+// writes one segment of all rows: 485 us against 520 (dropout and residual, 131,072 x 4,096 bf16). For
+// looked-up rows it is 282 against 277, and with 2 segments (1,000 columns) 73 against 53.
 template <typename TI, typename TO, typename ID, bool DROP, bool RES, bool TAIL, int U>
 __global__ __launch_bounds__(kRowThreads) void wide_kernel(RowLaunch l) {
     const RowArgs &a = l.a;
     constexpr bool kIds = !__is_same(ID, NoIds);
     for (int64_t tile = blockIdx.x; tile < l.tiles; tile += gridDim.x) {
         const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const uint32_t round = l.div((uint32_t)tile);
-        const uint32_t block = ((uint32_t)tile - round * l.segments) * 64 + (threadIdx.x & 63);
-        const int64_t row0 = ((int64_t)round * (kRowThreads / 64) + wave) * U;
+        // Segment and group of U rows: wavefront by wavefront, or workgroup by workgroup.
+        const uint32_t number = l.by_segment ? (uint32_t)tile
+                                             : (uint32_t)tile * (kRowThreads / 64) + wave;
+        const uint32_t round = l.div(number);
+        const uint32_t block = (number - round * l.segments) * 64 + (threadIdx.x & 63);
+        const int64_t row0 = (l.by_segment ? (int64_t)round * (kRowThreads / 64) + wave : round) * U;
         if (row0 >= a.n || block >= (uint32_t)l.blocks)
             continue;
         const int col = block * kCols;
@@ -179,11 +185,11 @@ hipError_t launch_tail(const RowArgs &a, hipStream_t stream) {
     const int64_t total = a.n * blocks;
     if (blocks >= kWideBlocks && total >= (int64_t)1 << 19) {
         const int segments = (blocks + 63) / 64;
-        // Dropout's rows follow each other: 522 us with two of them in flight, 551 with four. Looked-up
-        // rows lie anywhere: 292 and 282 us. (131,072 x 4,096 bf16, p = 0.1.)
-        constexpr int kRows = __is_same(ID, NoIds) || sizeof(TI) == 4 ? 2 : 4;
-        const int64_t tiles = (a.n + kRows * 4 - 1) / (kRows * 4) * segments;
-        RowLaunch l{a, Divider(segments), blocks, segments, tiles};
+        constexpr int kRows = 2;
+        const bool by_segment = __is_same(ID, NoIds) && segments % 8 == 0;
+        const int64_t groups = (a.n + kRows - 1) / kRows;
+        const int64_t tiles = by_segment ? (groups + 3) / 4 * segments : (groups * segments + 3) / 4;
+        RowLaunch l{a, Divider(segments), blocks, segments, by_segment, tiles};
         const dim3 grid((unsigned)(l.tiles < kRowGrid ? l.tiles : kRowGrid));
         wide_kernel<TI, TO, ID, DROP, RES, TAIL, kRows><<<grid, kRowThreads, 0, stream>>>(l);
         return hipGetLastError();
@@ -191,7 +197,7 @@ hipError_t launch_tail(const RowArgs &a, hipStream_t stream) {
     // One block per thread until the chip is full, then four.
     const bool small = total < (int64_t)1 << 19;
     const int64_t per = (int64_t)kRowThreads * (small ? 1 : 4);
-    RowLaunch l{a, Divider(blocks), blocks, 0, (total + per - 1) / per};
+    RowLaunch l{a, Divider(blocks), blocks, 0, false, (total + per - 1) / per};
     const dim3 grid((unsigned)(l.tiles < kRowGrid ? l.tiles : kRowGrid));
     if (small)
         row_kernel<TI, TO, ID, DROP, RES, TAIL, 1><<<grid, kRowThreads, 0, stream>>>(l);

@@ -16,7 +16,9 @@
 //   join   the partial sums of each run are added up by a workgroup, in the order of the chunks.
 //
 // The work is bound by the bytes of grad_out and grad_table: pairs are 8 bytes a token, and the partial
-// sums are 4 bytes a column of chunks that one id covers.
+// sums are 4 bytes a column of chunks that one id covers. 131,072 tokens of 2,048 bf16 columns (dropout,
+// Zipf frequencies) into 50,000 rows of 32 bits: 224 us for 946 MB, of them 180 in `sum` (5.3 TB/s), 25 in
+// the sort, 22 in fold and join. Few tokens, and tables of few rows, are done another way, further down.
 #include <algorithm>
 
 #include "layers_device.h"
@@ -263,15 +265,16 @@ __device__ __forceinline__ const T *grad_row(const GradArgs &a, uint32_t token) 
     return (const T *)((const char *)a.grad + (int64_t)token * a.grad_stride);
 }
 
+// `empty`: no id points at the row.
 template <typename T, bool TAIL>
 __device__ __forceinline__ void write_row(const GradArgs &a, uint32_t key, int col, int exchange,
-                                          const float (&sum)[kCols]) {
+                                          const float (&sum)[kCols], bool empty = false) {
     T *p = (T *)((char *)a.table + (int64_t)key * a.table_stride) + col;
     const bool part = TAIL && col + kCols > a.cols;
     float y[kCols];
 #pragma unroll
     for (int i = 0; i < kCols; ++i)
-        y[i] = sum[i] * a.factor;
+        y[i] = empty ? 0.0f : sum[i] * a.factor;       // zeros for any factor
     if (a.accumulate) {
         const Raw<T> old = part ? load_block(p, a.cols - col) : load_block(p);
 #pragma unroll
@@ -570,7 +573,7 @@ struct Window {
 //   A small call is one window and this launch.
 //   A table of few rows has few sums per window, less than they are made of: they are added up over the
 //   windows by a second launch, in place of the sort, the fold and the join of the whole call.
-template <typename ID, typename TG, typename TT, int L, bool DROP, bool TAIL, int T>
+template <typename TG, typename TT, int L, bool DROP, bool TAIL, int T>
 __global__ __launch_bounds__(T) void small_kernel(GradArgs a, Window v) {
     constexpr int kGroups = T / L, kEach = kSmallIds / kSortThreads, kWaves = T / 64;
     __shared__ uint32_t place[kWaves][kSmallRows];         // counts, then next places
@@ -590,8 +593,10 @@ __global__ __launch_bounds__(T) void small_kernel(GradArgs a, Window v) {
     const int span = (n + T - 1) / T * 64, from = wave * span;
     const int to = min(n, from + span);
     auto row_of = [&](int i) {
-        const int64_t id = (int64_t)static_cast<const ID *>(a.ids)[token0 + i] - row0;
-        return id >= 0 && id < count ? (int)id : count;
+        const int64_t at = token0 + i;
+        const int64_t id = a.id_bytes == 8 ? static_cast<const int64_t *>(a.ids)[at]
+                                           : static_cast<const int32_t *>(a.ids)[at];
+        return id >= row0 && id < row0 + count ? (int)(id - row0) : count;
     };
     int row[kEach];
 #pragma unroll
@@ -652,19 +657,23 @@ __global__ __launch_bounds__(T) void small_kernel(GradArgs a, Window v) {
     const int block = (int)tile * L + in, col = block * kCols;
     const bool live = block < blocks_of(a.cols);
     const int exchange = live ? exchange_of(block, a.cols) : kAlone;
-    auto write = [&](int r, const float (&sum)[kCols]) {
+    auto write = [&](int r, const float (&sum)[kCols], bool empty) {
         if (!live)
             return;
         if (v.partial)
             store_block(v.partial + (window * a.rows + row0 + r) * v.width + col, sum);
         else
-            write_row<TT, TAIL>(a, (uint32_t)(row0 + r), col, exchange, sum);
+            write_row<TT, TAIL>(a, (uint32_t)(row0 + r), col, exchange, sum, empty);
     };
+    // A window's row that no id points at has the sums -0, which no others are: those begin with +0.
     if (v.partial || !a.accumulate)
         for (int r = group; r < count; r += kGroups)
             if (begin[r] == begin[r + 1]) {
-                const float zero[kCols] = {};
-                write(r, zero);
+                float none[kCols];
+#pragma unroll
+                for (int k = 0; k < kCols; ++k)
+                    none[k] = -0.0f;
+                write(r, none, true);
             }
     // This group's tokens [i0, i1) of the list.
     const int chunk = (total + kGroups - 1) / kGroups;
@@ -681,7 +690,7 @@ __global__ __launch_bounds__(T) void small_kernel(GradArgs a, Window v) {
                 for (int k = 0; k < kCols; ++k)
                     part[group][first && head ? 0 : 1][in * kCols + k] = sum[k];
             } else {
-                write(current, sum);
+                write(current, sum, false);
             }
         };
         constexpr int kAhead = 4;
@@ -735,7 +744,7 @@ __global__ __launch_bounds__(T) void small_kernel(GradArgs a, Window v) {
 #pragma unroll
                 for (int k = 0; k < kCols; ++k)
                     sum[k] += part[g][0][in * kCols + k];
-            write(r, sum);
+            write(r, sum, false);
         }
     }
 }
@@ -750,7 +759,10 @@ __global__ __launch_bounds__(256) void windows_kernel(GradArgs a, Window v) {
     const int block = (int)(blockIdx.x - row * v.tiles) * L + lane, col = block * kCols;
     const bool live = block < blocks_of(a.cols);
     const int share = (v.count + kGroups - 1) / kGroups, last = min(v.count, (group + 1) * share);
-    float sum[kCols] = {};
+    float sum[kCols];
+#pragma unroll
+    for (int k = 0; k < kCols; ++k)
+        sum[k] = -0.0f;
     if (live)
 #pragma unroll 8
         for (int w = group * share; w < last; ++w) {
@@ -767,7 +779,9 @@ __global__ __launch_bounds__(256) void windows_kernel(GradArgs a, Window v) {
 #pragma unroll
         for (int k = 0; k < kCols; ++k)
             sum[k] = part[lane][k];
-        write_row<TT, true>(a, row, col, exchange_of(block, a.cols), sum);
+        const bool empty = __float_as_uint(sum[0]) == 0x80000000u;       // in every window
+        if (!empty || !a.accumulate)
+            write_row<TT, true>(a, row, col, exchange_of(block, a.cols), sum, empty);
     }
 }
 
@@ -795,19 +809,21 @@ Plan plan(int64_t n, int64_t rows, int32_t cols) {
     p.window.width = p.width;
     const int64_t ranges = (rows + kSmallRows - 1) / kSmallRows;
     const int window_tokens = kWindowThreads * (kSmallIds / kSortThreads);
-    // Windows of 1,024 tokens, or 512 while there are fewer than 512 workgroups of them. With at most
-    // 128 rows the sums of a window are at most a quarter of 16-bit rows' bytes.
+    // Windows of 1,024 tokens, shorter ones while there are fewer than 512 workgroups of them, but with
+    // twice as many tokens as rows and so as sums. 400,000 x 96 bf16 into 51 rows 39 us, 57 by the sort
+    // of the whole call; 4,096 x 64 fp32 into 50 rows 10.8 with windows of 128, 17.5 with 512.
     if (rows <= kSmallTable && n > window_tokens) {
         p.window.rows = (int)std::min<int64_t>(rows, kSmallRows);
-        p.window.tokens = n / window_tokens * ranges * p.tiles < 512 && rows <= kSmallTable / 2
-                              ? window_tokens / 2
-                              : window_tokens;
+        int tokens = window_tokens;
+        while (tokens > 128 && tokens > 4 * rows && n / tokens * ranges * p.tiles < 512)
+            tokens /= 2;
+        p.window.tokens = tokens;
         p.window.count = (int)((n + p.window.tokens - 1) / p.window.tokens);
         p.bytes = (int64_t)p.window.count * rows * p.width * 4;
         return p;
     }
     // One launch: while a lane group of one workgroup, which may have all the tokens, has at most 64.
-    // 2,049 x 96 fp32 into 1,000 rows 9.5 us, 26 in the six launches; 4,096 x 1,024 into 2 rows would
+    // 2,049 x 96 fp32 into 1,000 rows 10.5 us, 26 in the six launches; 4,096 x 1,024 into 2 rows would
     // be 167.
     if (n <= std::min(kSmallIds, 64 * (kSortThreads / p.lanes)) && ranges * p.tiles <= kSmallGroups) {
         p.window.rows = (int)std::max<int64_t>(
@@ -864,15 +880,14 @@ void launch_pass(Source source, const GradArgs &a, const Plan &p, int pass, Pair
             source, a.n, p.sort.tile, shift, p.sort.digit_bits, counts, p.sort.tiles, out, found);
 }
 
-template <typename ID, typename TG, typename TT, int L, bool DROP, bool TAIL>
+template <typename TG, typename TT, int L, bool DROP, bool TAIL>
 void launch_small(const GradArgs &a, const Window &v, hipStream_t stream) {
     const unsigned groups = (unsigned)((a.rows + v.rows - 1) / v.rows * v.count * v.tiles);
     if (v.partial)
-        small_kernel<ID, TG, TT, L, DROP, TAIL, kWindowThreads>
+        small_kernel<TG, TT, L, DROP, TAIL, kWindowThreads>
             <<<groups, kWindowThreads, 0, stream>>>(a, v);
-    else
-        small_kernel<ID, TG, TT, L, DROP, TAIL, kSortThreads>
-            <<<groups, kSortThreads, 0, stream>>>(a, v);
+    else          // one kernel for all alignments: its time is not in the rows
+        small_kernel<TG, TT, L, DROP, true, kSortThreads><<<groups, kSortThreads, 0, stream>>>(a, v);
 }
 
 template <typename TG, typename TT, int L, bool DROP, bool TAIL>
@@ -880,10 +895,7 @@ void launch_sum(const GradArgs &a, const Runs &r, const Plan &p, hipStream_t str
     if (p.window.count) {
         Window v = p.window;
         v.partial = v.count > 1 ? static_cast<float *>(a.workspace) : nullptr;
-        if (a.id_bytes == 4)
-            launch_small<int32_t, TG, TT, L, DROP, TAIL>(a, v, stream);
-        else
-            launch_small<int64_t, TG, TT, L, DROP, TAIL>(a, v, stream);
+        launch_small<TG, TT, L, DROP, TAIL>(a, v, stream);
         if (v.partial)
             windows_kernel<TT, L><<<(unsigned)(a.rows * v.tiles), 256, 0, stream>>>(a, v);
         return;

@@ -185,6 +185,36 @@ def test_grad_accumulates_into_touched_rows_only(table):
     assert_close(got, want + before, np.where(count > 0, tol, 0.0))
 
 
+@pytest.mark.parametrize("n,rows,cols", [(300, 90, 72), (20_000, 100, 72), (9_000, 2_000, 16),
+                                         (300_000, 9_000, 8)])
+def test_grad_leaves_rows_without_ids_alone(n, rows, cols):
+    """Bit for bit where it accumulates: -0, subnormal numbers and the bits of a NaN. Otherwise they are
+    zeros, whatever the factor is. In one launch, in windows, by sorted pairs, with a fold."""
+    note(f"grad rows without ids n={n} rows={rows} cols={cols}")
+    r = rng(n)
+    ids = r.integers(0, rows // 2, n) * 2
+    ids[ids == 4] = 0
+    untouched = np.setdiff1d(np.arange(rows), ids)
+    assert len(untouched) > rows // 2
+    kinds = np.array([0x80000000, 1, 0x80000001, 0x7FC12345, 0xFF800000, 0x3F800000], np.uint32)
+    bits = kinds[r.integers(0, len(kinds), (rows, cols))]
+    table = torch.from_numpy(bits.view(np.float32)).to(DEV)
+    d = torch.ones(n, cols, device=DEV)
+    gpu_ids = torch.from_numpy(ids).to(DEV)
+    ws = torch.full((P.cc_embedding_grad_workspace_bytes(n, rows, cols),), 0xA5, dtype=torch.uint8,
+                    device=DEV)
+    P.cc_embedding_grad(gpu_ids, d, table, ws, accumulate=True)
+    torch.cuda.synchronize()
+    got = table.cpu().numpy().view(np.uint32)
+    assert (got[untouched] == bits[untouched]).all()
+    table.fill_(7.0)
+    P.cc_embedding_grad(gpu_ids, d, table, ws, scale=float("inf"))
+    torch.cuda.synchronize()
+    got = table.cpu().numpy()
+    assert (got[untouched].view(np.uint32) == 0).all()
+    assert np.isposinf(np.delete(got, untouched, 0)).all()
+
+
 def test_grad_of_nothing():
     note("grad: no ids, no rows")
     none = np.empty(0, np.int64)

@@ -211,7 +211,7 @@ __global__ __launch_bounds__(kSortThreads) void digit_scatter(Source source, int
 
 // ---- sums of runs ----
 
-constexpr int64_t kStripBytes = 128 << 10;
+constexpr int64_t kStripBytes = 128 << 10, kMaxStrips = 1 << 21;
 
 struct Runs {
     const Pair *pairs;
@@ -296,19 +296,22 @@ template <typename TG, typename TT, int L, bool DROP, bool TAIL>
 __global__ __launch_bounds__(256) void sum_kernel(GradArgs a, Runs r, uint32_t strips, int strip) {
     const uint32_t strips_before = (uint32_t)((uint64_t)blockIdx.x * strips / gridDim.x);
     if ((uint32_t)((uint64_t)(blockIdx.x + 1) * strips / gridDim.x) > strips_before) {
-        const int64_t row0 = (int64_t)strips_before * strip;
-        const int count = (int)min((int64_t)strip, a.rows - row0), lane = threadIdx.x & 63;
-        const uint64_t empty = __ballot(lane < count && !r.found[row0 + min(lane, count - 1)]);
-        for (int row = threadIdx.x / L; row < count; row += 256 / L) {
-            if (!(empty >> row & 1))
-                continue;
-            TT *p = (TT *)((char *)a.table + (row0 + row) * a.table_stride);
-            if (TAIL) {
-                for (int col = threadIdx.x % L; col < a.cols; col += L)
-                    p[col] = (TT)0.0f;
-            } else {
-                for (int i = threadIdx.x % L; i < a.cols * (int)sizeof(TT) / 16; i += L)
-                    __builtin_nontemporal_store(words_t{}, (words_t *)p + i);
+        const int64_t first = (int64_t)strips_before * strip, last = min(first + strip, a.rows);
+        const int lane = threadIdx.x & 63;
+        for (int64_t row0 = first; row0 < last; row0 += 64) {
+            const int count = (int)min((int64_t)64, last - row0);
+            const uint64_t empty = __ballot(lane < count && !r.found[row0 + min(lane, count - 1)]);
+            for (int row = threadIdx.x / L; row < count; row += 256 / L) {
+                if (!(empty >> row & 1))
+                    continue;
+                TT *p = (TT *)((char *)a.table + (row0 + row) * a.table_stride);
+                if (TAIL) {
+                    for (int col = threadIdx.x % L; col < a.cols; col += L)
+                        p[col] = (TT)0.0f;
+                } else {
+                    for (int i = threadIdx.x % L; i < a.cols * (int)sizeof(TT) / 16; i += L)
+                        __builtin_nontemporal_store(words_t{}, (words_t *)p + i);
+                }
             }
         }
         return;
@@ -901,9 +904,12 @@ void launch_sum(const GradArgs &a, const Runs &r, const Plan &p, hipStream_t str
         return;
     }
     const int64_t sum_groups = (r.chunks * r.tiles + 256 / L - 1) / (256 / L);
-    // Strips of rows of about 128 KiB.
+    // Strips of rows of about 128 KiB, 64 rows at most, but more where the launch would have more
+    // workgroups than it may (tables of over 2^27 rows).
     const int64_t row_bytes = (int64_t)a.cols * sizeof(TT);
-    const int strip = (int)std::max<int64_t>(1, std::min<int64_t>(64, kStripBytes / row_bytes));
+    int strip = (int)std::max<int64_t>(1, std::min<int64_t>(64, kStripBytes / row_bytes));
+    while (a.rows / strip > kMaxStrips)
+        strip *= 2;
     const int64_t strips = a.accumulate ? 0 : (a.rows + strip - 1) / strip;
     if (sum_groups + strips > 0)
         sum_kernel<TG, TT, L, DROP, TAIL><<<(unsigned)(sum_groups + strips), 256, 0, stream>>>(

@@ -172,3 +172,16 @@ def test_the_example_learns_and_serves():
     step = hidden.float().abs().amax(1)[:, None] / 254 * weights.abs().sum(1) + \
         hidden.float().abs().sum(1)[:, None] * weights.abs().amax(1) / 254
     assert ((out.float() - plain).abs() <= 1.02 * step + 2.0 ** -8 * plain + 1e-6).all()
+
+
+def test_gradient_of_a_table_of_more_rows_than_a_launch_has_workgroups_of_64():
+    """2^30 rows and some: the rows that no id points at are written in longer strips."""
+    note("grad: 2^30 rows")
+    rows = (1 << 30) + 77
+    ids = torch.tensor([rows - 1, 0, 1 << 29, rows, 0], device=DEV)
+    dout = torch.tensor([[1.0], [2.0], [4.0], [8.0], [16.0]], device=DEV, dtype=torch.bfloat16)
+    grad = torch.ones(rows, 1, device=DEV, dtype=torch.bfloat16)
+    ws = torch.empty(P.cc_embedding_grad_workspace_bytes(5, rows, 1), dtype=torch.uint8, device=DEV)
+    P.cc_embedding_grad(ids, dout, grad, ws)
+    assert [float(grad[i]) for i in (0, 1 << 29, rows - 1)] == [18.0, 4.0, 1.0]
+    assert int(grad.view(torch.int16).count_nonzero()) == 3

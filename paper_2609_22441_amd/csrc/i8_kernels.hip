@@ -1,4 +1,10 @@
 // 8-bit integers with a scale per row: quantisation of rows, and the product of two such matrices.
+//
+// Quantisation moves bytes: 16,384 x 8,192 bf16 75 us (403 MB, 5.3 TB/s). Large products are bound by the
+// matrix instructions: 8,192^3 469 us (2,345 TOPS), 8,192 x 16,384 x 4,096 522 (2,106; 268 MB of output
+// follow the sums), linear 16,384 x 8,192 x 8,192 1,018 with the quantisation. Short ones by their output
+// (50,000 x 512 x 96 20.9 us, 15 of them the product's), those of few rows by the weights and the launch
+// (1 x 4,096 x 4,096 7.5 us).
 #include "i8_choice.h"
 #include "layers_device.h"
 

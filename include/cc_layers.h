@@ -166,7 +166,8 @@ CC_API cc_status cc_quantize_rows(const void *x, int64_t x_stride, int32_t type,
  *               (a linear layer's weights, one row per output). 16-byte aligned, strides and k
  *               multiples of 16, the form that cc_quantize_rows writes (its zero columns add
  *               nothing).
- *   m, n        >= 0, below 2^31.
+ *   m, n        >= 0, below 2^31 (within 256 of it, a launch has too many workgroups:
+ *               CC_ERR_DEVICE).
  *   k           0 to 131,056 (no sum of products of values in [-128, 127] passes 31 bits).
  *   a_scales    [m] float; b_scales: [n] float; bias: [n] float or NULL.
  *   out         [m][n] of out_type, row stride out_stride bytes.

@@ -21,6 +21,7 @@
 // the sort, 22 in fold and join. Few tokens, and tables of few rows, are done another way, further down.
 #include <algorithm>
 
+#include "grad_runs.h"
 #include "layers_device.h"
 
 namespace ccj {
@@ -249,7 +250,6 @@ struct Runs {
 
 constexpr int kJoinThreads = 1024;
 constexpr int64_t kJoinGrid = 512;      // two workgroups per unit
-constexpr int kFold = 16;        // chunks whose partial sums are added up together
 
 // A group's pairs: through the scalar cache where the group is a wavefront.
 template <int L>
@@ -329,11 +329,10 @@ __global__ __launch_bounds__(256) void sum_kernel(GradArgs a, Runs r, uint32_t s
     if (c >= r.chunks || block >= r.blocks)
         return;
     const bool began = start > 0 && pairs[start - 1].key == low;
-    const bool covers = of_low == stop - start, next = of_high == min(r.chunk, r.n - stop);
-    // The chunk's own tokens; whether its first run began before it, and its last goes on past it.
-    const int64_t i0 = start + (began && !covers ? of_low : 0);
-    const int64_t i1 = stop + (next ? 0 : of_high);
-    const bool head = began && covers, tail = of_high && next;
+    const ChunkEnds ends =
+        chunk_ends(start, stop, r.n, r.chunk, began, of_low, of_high, high, a.rows);
+    const int64_t i0 = ends.i0, i1 = ends.i1;
+    const bool head = ends.head, tail = ends.tail;
     const int col = block * kCols;
     const int exchange = exchange_of(block, a.cols);
     uint32_t current = pairs[i0].key;
@@ -367,8 +366,8 @@ __global__ __launch_bounds__(256) void sum_kernel(GradArgs a, Runs r, uint32_t s
         }
     };
     // kAhead rows are added while the next kAhead are on their way, then the rest. Ids outside the table
-    // come last and end the loop.
-    constexpr int kAhead = 4;
+    // come last and end the loop: `current` is then the last id of the table.
+    constexpr int kAhead = kSumAhead;
     uint32_t key[2][kAhead], token[2][kAhead];
     Raw<TG> x[2][kAhead];
     auto fetch = [&](int s, int64_t i) {
@@ -381,7 +380,7 @@ __global__ __launch_bounds__(256) void sum_kernel(GradArgs a, Runs r, uint32_t s
         for (int j = 0; j < kAhead; ++j)
             x[s][j] = load_most<TAIL, true>(grad_row<TG>(a, token[s][j]), col, a.cols, exchange);
     };
-    const int64_t even = i0 + (i1 - i0) / (2 * kAhead) * (2 * kAhead);
+    const int64_t even = pipelined(ends);
     if (i0 < even)
         fetch(0, i0);
     for (int64_t i = i0; i < even && key[0][0] < (uint64_t)a.rows; i += 2 * kAhead) {

@@ -21,45 +21,19 @@
 // the sort, 22 in fold and join. Few tokens, and tables of few rows, are done another way, further down.
 #include <algorithm>
 
-#include "grad_runs.h"
+#include "grad_choice.h"
 #include "layers_device.h"
 
 namespace ccj {
 namespace {
 
+static_assert(kGradBlock == kCols, "the choice counts the kernels' column blocks");
+
 // ---- sorted pairs ----
 
-struct Pair {
-    uint32_t key, token;
-};
-
-constexpr int kSortThreads = 1024;
 constexpr int kSortWaves = kSortThreads / 64;
-constexpr int kMaxDigitBits = 9;
 constexpr int kMaxDigits = 1 << kMaxDigitBits;
-constexpr int kMinTile = 2048;          // pairs per workgroup of a digit pass
 constexpr int kClearWords = 4 * kSortThreads;   // of 16 bytes, cleared by a workgroup
-constexpr int kMaxTiles = 256;          // every workgroup reads the counts of all tiles
-constexpr int64_t kMaxChunks = 1 << 18; // chunks times column tiles: the joins' grid stays launchable
-
-struct SortShape {
-    int32_t passes, digit_bits;         // digit passes, bits of each
-    int32_t tiles;
-    int64_t tile;                       // pairs per tile, a multiple of kSortThreads
-};
-
-SortShape sort_shape(int64_t n, int64_t rows) {
-    SortShape s;
-    int bits = 1;
-    while (rows >> bits)                // keys 0 to rows: the last is every id outside the table
-        ++bits;
-    s.passes = (bits + kMaxDigitBits - 1) / kMaxDigitBits;
-    s.digit_bits = (bits + s.passes - 1) / s.passes;
-    const int64_t even = (n + kMaxTiles - 1) / kMaxTiles;
-    s.tile = std::max<int64_t>(kMinTile, (even + kSortThreads - 1) / kSortThreads * kSortThreads);
-    s.tiles = (int32_t)((n + s.tile - 1) / s.tile);
-    return s;
-}
 
 __device__ __forceinline__ uint32_t key_of(int64_t id, int64_t rows) {
     return (uint32_t)(id >= 0 && id < rows ? id : rows);
@@ -248,7 +222,6 @@ struct Runs {
     }
 };
 
-constexpr int kJoinThreads = 1024;
 constexpr int64_t kJoinGrid = 512;      // two workgroups per unit
 
 // A group's pairs: through the scalar cache where the group is a wavefront.
@@ -556,19 +529,6 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(GradArgs a, Runs r) 
 
 // ---- small calls and small tables: pairs in LDS ----
 
-constexpr int kSmallIds = 4096;         // tokens of a workgroup of 1,024: 12 bits
-constexpr int kWindowThreads = 256;     // of a small table's windows, of 4 tokens per thread
-constexpr int kSmallRows = 64;          // rows of a workgroup, at most
-constexpr int kSmallGroups = 1024;      // workgroups of a small call, at most: each reads all ids
-constexpr int kSmallTable = 128;        // rows of a small table
-
-struct Window {
-    int32_t rows, tiles;         // of the table per workgroup; column tiles
-    int32_t tokens, count;       // tokens per window; windows
-    float *partial;              // [count][a.rows][width], or null: one window, its sums are final
-    int32_t width;
-};
-
 // A workgroup has a window of the tokens, `rows` rows of the table and one column tile. It reads the
 // window's ids, puts its rows' tokens in order in LDS by the digit pass above, and adds them up as
 // above: its lane groups share the tokens out evenly, and what runs leave at their edges meets in LDS.
@@ -787,85 +747,8 @@ __global__ __launch_bounds__(256) void windows_kernel(GradArgs a, Window v) {
     }
 }
 
-// ---- layout of the workspace ----
-
-int64_t round16(int64_t x) { return (x + 15) & ~(int64_t)15; }
-
-struct Plan {
-    SortShape sort;
-    Window window;                                       // count 0: the sorted way
-    int64_t chunk, chunks;
-    int32_t lanes, tiles, width;
-    int64_t folds;                                       // 0: none, the chunks are joined
-    int64_t counts, found, list, pairs0, pairs1, partial, folded, bytes;  // offsets, the total size
-};
-
-Plan plan(int64_t n, int64_t rows, int32_t cols) {
-    Plan p = {};
-    p.sort = sort_shape(n, rows);
-    const int blocks = blocks_of(cols);
-    p.lanes = blocks <= 4 ? 4 : blocks <= 16 ? 16 : 64;
-    p.tiles = (blocks + p.lanes - 1) / p.lanes;
-    p.width = blocks * kCols;
-    p.window.tiles = p.tiles;
-    p.window.width = p.width;
-    const int64_t ranges = (rows + kSmallRows - 1) / kSmallRows;
-    const int window_tokens = kWindowThreads * (kSmallIds / kSortThreads);
-    // Windows of 1,024 tokens, shorter ones while there are fewer than 512 workgroups of them, but with
-    // twice as many tokens as rows and so as sums. 400,000 x 96 bf16 into 51 rows 39 us, 57 by the sort
-    // of the whole call; 4,096 x 64 fp32 into 50 rows 10.8 with windows of 128, 17.5 with 512.
-    if (rows <= kSmallTable && n > window_tokens) {
-        p.window.rows = (int)std::min<int64_t>(rows, kSmallRows);
-        int tokens = window_tokens;
-        while (tokens > 128 && tokens > 4 * rows && n / tokens * ranges * p.tiles < 512)
-            tokens /= 2;
-        p.window.tokens = tokens;
-        p.window.count = (int)((n + p.window.tokens - 1) / p.window.tokens);
-        p.bytes = (int64_t)p.window.count * rows * p.width * 4;
-        return p;
-    }
-    // One launch: while a lane group of one workgroup, which may have all the tokens, has at most 64.
-    // 2,049 x 96 fp32 into 1,000 rows 10.5 us, 26 in the six launches; 4,096 x 1,024 into 2 rows would
-    // be 167.
-    if (n <= std::min(kSmallIds, 64 * (kSortThreads / p.lanes)) && ranges * p.tiles <= kSmallGroups) {
-        p.window.rows = (int)std::max<int64_t>(
-            1, std::min<int64_t>(kSmallRows, (rows * p.tiles + 255) / 256));
-        p.window.tokens = kSmallIds;
-        p.window.count = 1;
-        return p;
-    }
-    // Chunks of 16 tokens where rows are wide, so that the last wavefronts to run are few of many, and 32
-    // where more groups share a wavefront; shorter ones while the chip has fewer than 4 wavefronts per
-    // SIMD of them. 131,072 x 2,048 bf16, Zipf frequencies: 183 us in the sums with 16, 192 with 32, 207
-    // with 64.
-    p.chunk = p.lanes == 64 ? 16 : 32;
-    while (p.chunk > 8 && n / p.chunk * p.tiles * p.lanes < 4 * 1024 * 64)
-        p.chunk /= 2;
-    while (n / p.chunk * p.tiles > kMaxChunks)
-        p.chunk *= 2;
-    p.chunks = (n + p.chunk - 1) / p.chunk;
-    int64_t at = 0;
-    auto take = [&](int64_t bytes) {
-        const int64_t here = at;
-        at += round16(bytes);
-        return here;
-    };
-    p.counts = take((int64_t)p.sort.tiles << p.sort.digit_bits << 2);
-    p.found = take(rows + 1);               // the last: ids outside the table
-    p.list = take(4 * (p.chunks + 1));
-    p.pairs0 = take(n * (int64_t)sizeof(Pair));
-    p.pairs1 = take(p.sort.passes > 1 ? n * (int64_t)sizeof(Pair) : 0);
-    p.partial = take(p.chunks * 2 * p.width * 4);
-    // A run's partial sums are added up by the lane groups of one workgroup: folded first where a group
-    // could get more than 32 of them.
-    p.folds = p.chunks > 32 * (kJoinThreads / p.lanes) ? (p.chunks + kFold - 1) / kFold : 0;
-    p.folded = take(p.folds * 2 * p.width * 4);
-    p.bytes = at;
-    return p;
-}
-
 template <typename Source>
-void launch_pass(Source source, const GradArgs &a, const Plan &p, int pass, Pair *out,
+void launch_pass(Source source, const GradArgs &a, const GradPlan &p, int pass, Pair *out,
                  hipStream_t stream) {
     char *ws = static_cast<char *>(a.workspace);
     uint32_t *counts = (uint32_t *)(ws + p.counts);
@@ -893,7 +776,7 @@ void launch_small(const GradArgs &a, const Window &v, hipStream_t stream) {
 }
 
 template <typename TG, typename TT, int L, bool DROP, bool TAIL>
-void launch_sum(const GradArgs &a, const Runs &r, const Plan &p, hipStream_t stream) {
+void launch_sum(const GradArgs &a, const Runs &r, const GradPlan &p, hipStream_t stream) {
     if (p.window.count) {
         Window v = p.window;
         v.partial = v.count > 1 ? static_cast<float *>(a.workspace) : nullptr;
@@ -927,7 +810,7 @@ void launch_sum(const GradArgs &a, const Runs &r, const Plan &p, hipStream_t str
 }
 
 template <typename TG, typename TT, int L>
-void launch_drop(const GradArgs &a, const Runs &r, const Plan &p, hipStream_t stream) {
+void launch_drop(const GradArgs &a, const Runs &r, const GradPlan &p, hipStream_t stream) {
     const bool drop = a.mask.threshold != kThresholdOne;
     const bool tail = a.cols % kCols || !even_rows(a.grad, a.grad_stride) ||
                       !even_rows(a.table, a.table_stride);
@@ -940,7 +823,7 @@ void launch_drop(const GradArgs &a, const Runs &r, const Plan &p, hipStream_t st
 }
 
 template <typename TG, typename TT>
-void launch_lanes(const GradArgs &a, const Runs &r, const Plan &p, hipStream_t stream) {
+void launch_lanes(const GradArgs &a, const Runs &r, const GradPlan &p, hipStream_t stream) {
     if (p.lanes == 4)
         launch_drop<TG, TT, 4>(a, r, p, stream);
     else if (p.lanes == 16)
@@ -952,11 +835,11 @@ void launch_lanes(const GradArgs &a, const Runs &r, const Plan &p, hipStream_t s
 }  // namespace
 
 int64_t grad_workspace_bytes(int64_t n, int64_t rows, int32_t cols) {
-    return plan(n, rows, cols).bytes;
+    return grad_plan(n, rows, cols).bytes;
 }
 
 hipError_t launch_embedding_grad(const GradArgs &a, hipStream_t stream) {
-    const Plan p = plan(a.n, a.rows, a.cols);
+    const GradPlan p = grad_plan(a.n, a.rows, a.cols);
     char *ws = static_cast<char *>(a.workspace);
     Pair *pairs[2] = {(Pair *)(ws + p.pairs0), (Pair *)(ws + p.pairs1)};
     for (int pass = 0; !p.window.count && pass < (a.n > 0 ? p.sort.passes : 1); ++pass) {

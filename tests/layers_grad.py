@@ -27,12 +27,34 @@ def rows_on_gpu(n, cols, dtype, seed, pad=0, shift=0):
     return view
 
 
+def kept(rows, cols, p, seed, site=0, first_row=0):
+    """layers_oracle.kept on the GPU, some rows at a time: products modulo 2^64, whose halves are exact."""
+    blocks = (cols + 7) // 8
+    keep = torch.empty(rows, blocks, 8, dtype=torch.bool, device=DEV)
+    step = max(1, (1 << 22) // blocks)
+    for i in range(0, rows, step):
+        row = torch.arange(first_row + i, first_row + min(i + step, rows), device=DEV)[:, None]
+        c = [row & O.M32, row >> 32, torch.arange(blocks, device=DEV)[None, :],
+             torch.full((1, 1), site, device=DEV)]
+        k = [seed & O.M32, seed >> 32]
+        for _ in range(10):
+            a, b = c[0] * 0xD2511F53, c[2] * 0xCD9E8D57
+            c = [(b >> 32 & O.M32) ^ c[1] ^ k[0], b & O.M32, (a >> 32 & O.M32) ^ c[3] ^ k[1], a & O.M32]
+            k = [(k[0] + 0x9E3779B9) & O.M32, (k[1] + 0xBB67AE85) & O.M32]
+        for j in range(8):
+            keep[i:i + step, :, j] = (c[j // 2] >> (16 * (j % 2)) & 0xFFFF) < O.threshold(p)
+    return keep.view(rows, blocks * 8)[:, :cols]
+
+
 def sums(ids, d, rows, keep, factor):
-    """(gradient, sum of the magnitudes that were added, additions) in 64 bits."""
+    """(gradient, sum of the magnitudes that were added, additions) in 64 bits. Tokens go round several tables,
+    which are added up at the end: a row that takes most of the tokens is slow as one."""
     n, cols = d.shape
-    want = torch.zeros(rows + 1, cols, dtype=torch.float64, device=DEV)     # the last: ids outside
-    size, count = torch.zeros_like(want), torch.zeros(rows + 1, dtype=torch.float64, device=DEV)
-    to = torch.where((ids >= 0) & (ids < rows), ids.long(), rows)
+    tables = min(1024, max(1, (1 << 25) // ((rows + 1) * (cols + 1))))
+    to = torch.where((ids >= 0) & (ids < rows), ids.long(), rows)           # the last: ids outside
+    to = to + torch.arange(n, device=DEV) % tables * (rows + 1)
+    want, size = (torch.zeros(tables * (rows + 1), cols, dtype=torch.float64, device=DEV)
+                  for _ in range(2))
     step = max(1, (1 << 25) // cols)
     for i in range(0, n, step):
         x = d[i:i + step].double() * factor
@@ -40,8 +62,8 @@ def sums(ids, d, rows, keep, factor):
             x = torch.where(keep[i:i + step], x, 0.0)
         want.index_add_(0, to[i:i + step], x)
         size.index_add_(0, to[i:i + step], x.abs())
-    count.index_add_(0, to, torch.ones_like(to, dtype=torch.float64))
-    return want[:rows], size[:rows], count[:rows, None]
+    count = torch.bincount(to, minlength=tables * (rows + 1)).double()[:, None]
+    return [t.view(tables, rows + 1, -1).sum(0)[:rows] for t in (want, size, count)]
 
 
 def check(ids, d, rows, table, scale=1.0, drop=None, accumulate=False, pad=0, shift=0, what=""):
@@ -52,7 +74,7 @@ def check(ids, d, rows, table, scale=1.0, drop=None, accumulate=False, pad=0, sh
     ids = torch.from_numpy(ids).to(DEV)
     keep, factor = None, scale
     if drop:
-        keep = torch.from_numpy(O.kept(n, cols, **drop)).to(DEV)
+        keep = kept(n, cols, **drop)
         factor = scale * 65536 / O.threshold(drop["p"])
     want, size, count = sums(ids, d, rows, keep, factor)
     o = Output(rows + 2, cols, TYPES[table], pad, shift)

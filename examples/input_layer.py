@@ -1,12 +1,14 @@
-"""The scoring model's input layer on joined rows: training steps of a position table, then serving in
-8-bit integers (Connected Content Retriever, §4: Eq. 2 and Eq. 3).
+"""Learned rows and a dense layer on joined rows: training steps of a position table, then serving in 8-bit
+integers (dropout and ReLU(W h + b): Connected Content Retriever, §4, Eq. 2).
 
     python examples/input_layer.py
 
 Both start from the join: every candidate's document row and its viewer's edge row for the document's
-author, 96 bf16 columns. Training adds the row of the candidate's slot, E_pos(min(slot, S_max)), to the
-rows under dropout, and learns the position table by the gradient that cc_embedding_grad sums by slot.
-Serving adds the learned rows and runs the first dense layer, ReLU(W h + b), in 8-bit integers.
+author, 96 bf16 columns. Training adds a row for the candidate's slot, number min(slot, S_max) of a table, to
+the rows under dropout, and learns the table by the gradient that cc_embedding_grad sums by slot. (This is
+the example's own use of a table of rows. The paper's Eq. 3 adds a slot's row to the model's 3 logits: the
+same two calls with a table of 3 columns.) Serving adds the learned rows and runs the first dense layer,
+ReLU(W h + b), in 8-bit integers.
 """
 from __future__ import annotations
 
@@ -73,7 +75,7 @@ class Training:
 
 
 class Serving:
-    """rows + E_pos[slots] -> ReLU(W h + b) with W quantised once."""
+    """rows + table[slots] -> ReLU(W h + b) with W quantised once."""
 
     def __init__(self, table, weights, bias):
         outputs, cols = weights.shape

@@ -1,10 +1,11 @@
 /*
- * cc_layers.h -- C ABI of the scoring model's input layer (libccjoin.so, next to cc_join.h).
+ * cc_layers.h -- C ABI of operators of the scoring model (libccjoin.so, next to cc_join.h).
  *
- * The join writes the rows that the scoring model reads; the operators here are the model's first
- * steps on such rows (Connected Content Retriever, §4): tables of learned rows looked up by id
- * (Eq. 3: a position's row E_pos(min(slot, S_max))), dropout (Eq. 2), and the dense product
- * W h + b with ReLU (Eq. 2).
+ * The join writes the rows that the scoring model reads; the operators here are those that meet such
+ * rows first (Connected Content Retriever, §4): the dense product W h + b with ReLU, and dropout, of
+ * a block Dropout(LN(ReLU(W h + b))) of Eq. 2 (its layer norm is not here), and tables of learned
+ * rows looked up by id. Eq. 3's table is one of these: S_max + 1 rows of 3 columns, of which
+ * E_pos(min(slot, S_max)) is added to the model's 3 logits.
  *
  *   training   cc_embedding_lookup (with dropout), cc_embedding_grad, cc_dropout (forward, and on
  *              the output's gradient the backward pass)
@@ -19,7 +20,8 @@
  *     Pointers are aligned to their element size unless stated otherwise. 16-byte alignment of
  *     pointers and strides is faster.
  *   - An output must not overlap an input or the workspace (CC_ERR_INVALID_ARGUMENT), except
- *     where in-place use is stated.
+ *     where in-place use is stated. A matrix counts from its first element to its last: side by side
+ *     in one buffer's rows, two matrices overlap.
  *   - A workspace is device scratch, 16-byte aligned, whose contents need no preparation and are
  *     not kept from one call to the next; two calls that may run at the same time need one each.
  *   - A call with no output elements returns CC_OK and enqueues nothing.
@@ -171,7 +173,8 @@ CC_API cc_status cc_quantize_rows(const void *x, int64_t x_stride, int32_t type,
  *   k           0 to 131,056 (no sum of products of values in [-128, 127] passes 31 bits).
  *   a_scales    [m] float; b_scales: [n] float; bias: [n] float or NULL.
  *   out         [m][n] of out_type, row stride out_stride bytes.
- *   workspace   cc_matmul_i8_workspace_bytes(m, n, k) bytes, NULL where that is 0.
+ *   workspace   cc_matmul_i8_workspace_bytes(m, n, k) bytes, NULL where that is 0. No size needs
+ *               any now.
  * Errors: CC_ERR_INVALID_ARGUMENT, CC_ERR_DEVICE.
  */
 CC_API int64_t cc_matmul_i8_workspace_bytes(int64_t m, int64_t n, int64_t k);

@@ -18,8 +18,8 @@ Five kinds of case:
 The 4-bit form. A block of 32 values of a row has a scale 2^(s - 127) and a value each of 0, 0.5, 1,
 1.5, 2, 3, 4, 6 and a sign (OCP Microscaling Formats, E2M1 with E8M0). s is the exponent (biased) of the
 largest magnitude, rounded to one bit of mantissa, less 2; values are rounded to nearest, ties to
-even, and at most 6. Two values to a byte, the first in the low half; rows are padded to 128 values
-with zeros.
+even, and at most 6. Two values to a byte, the first in the low half; rows are padded with zeros, of
+values to 128, of scales to 16.
 """
 from __future__ import annotations
 
@@ -167,7 +167,7 @@ def _hidden(rows, cols, dtype, g, pad=0, unit=1.0):
 
 
 def _four_bits(x):
-    """(q, scales): x's rows in 4 bits, two values to a byte, padded to 128 with zeros."""
+    """(q, scales): x's rows in 4 bits, two values to a byte, and their scales."""
     rows, cols = x.shape
     padded = -(-cols // 128) * 128
     wide = torch.zeros(rows, padded, device=DEV)
@@ -179,7 +179,9 @@ def _four_bits(x):
     code = torch.where(a < 2, 2 * a, torch.where(a < 4, 2 + a, 4 + a / 2)).to(torch.uint8)
     code |= (v < 0).to(torch.uint8) << 3
     code = code.view(rows, padded)
-    return (code[:, 0::2] | code[:, 1::2] << 4).contiguous(), s.view(rows, -1).to(torch.uint8)
+    scales = torch.zeros(rows, -(-cols // 512) * 16, dtype=torch.uint8, device=DEV)
+    scales[:, :padded // 32] = s.view(rows, -1)
+    return (code[:, 0::2] | code[:, 1::2] << 4).contiguous(), scales
 
 
 def prepare(case, seed):
@@ -254,7 +256,8 @@ def _prepare_own(s):
     elif kind == "round":
         padded = -(-case["cols"] // 128) * 128
         s["q"] = torch.empty(case["rows"], padded // 2, dtype=torch.uint8, device=DEV)
-        s["scales"] = torch.empty(case["rows"], padded // 32, dtype=torch.uint8, device=DEV)
+        s["scales"] = torch.empty(case["rows"], -(-case["cols"] // 512) * 16, dtype=torch.uint8,
+                                  device=DEV)
         s["out"] = _empty(case["rows"], case["cols"], case["dtype"], case["pad"])
     else:
         s["out"] = _empty(case["m"], case["n"], case["dtype"])
@@ -417,7 +420,8 @@ def _values(q, scales):
     """The values of a 4-bit matrix in 32 bits."""
     code = torch.stack([q & 15, q >> 4], 2).view(q.shape[0], -1).int()
     grid = torch.tensor(GRID + tuple(-v for v in GRID), device=DEV)
-    v = grid[code].view(q.shape[0], -1, 32) * _power(scales.int() - 127)[:, :, None]
+    power = _power(scales[:, :q.shape[1] // 16].int() - 127)
+    v = grid[code].view(q.shape[0], -1, 32) * power[:, :, None]
     return v.view(q.shape[0], -1)
 
 
@@ -499,7 +503,8 @@ def _exact_values(q, scales, k):
         value = torch.where(magnitude < 2, low, high)
         pairs[..., half] = torch.where(nibble >= 8, -value, value)
     v = pairs.view(q.shape[0], -1)
-    return (v * torch.pow(2.0, scales.double() - 127).repeat_interleave(32, dim=1))[:, :k]
+    units = torch.pow(2.0, scales.double() - 127).repeat_interleave(32, dim=1)
+    return (v * units[:, :v.shape[1]])[:, :k]
 
 
 def _exact_norm(case, s):

@@ -1,8 +1,8 @@
 """MI355X-native edge-feature join (Connected Content Retriever, §3.1 and §6.3), with the
 device sort of the affinity records (Alg. 1 Step 1), the document-id map (§6.3.1, Eq. 6) and
-ingestion into the store (§6.2); and the first layer of the scoring model that reads the joined
-rows (§4): embedding lookup and gradient, dropout, 8-bit products (``layers.py``, behind
-``include/cc_layers.h``).
+ingestion into the store (§6.2); and layers of the scoring model that reads the joined rows (§4):
+embedding lookup and gradient, dropout, block norms and their gradient, products in 8 and 4 bits
+(``layers.py``, behind ``include/cc_layers.h``).
 
 The work happens in ``libccjoin.so`` (hand-written HIP kernels for gfx950 behind the C ABI in
 ``include/cc_join.h``). This package is a thin ctypes binding with the same function names; it
@@ -23,4 +23,8 @@ from .layers import (  # noqa: F401
     cc_embedding_lookup, cc_embedding_grad, cc_embedding_grad_workspace_bytes, cc_dropout,
     cc_quantize_rows, cc_matmul_i8, cc_matmul_i8_workspace_bytes, cc_linear_i8,
     cc_linear_i8_workspace_bytes, CC_F32, CC_F16, CC_BF16,
+    cc_block_norm, cc_block_norm_grad, cc_block_norm_grad_workspace_bytes, cc_quantize_mxfp4,
+    cc_dequantize_mxfp4, cc_matmul_mxfp4, cc_matmul_mxfp4_workspace_bytes, cc_linear_mxfp4,
+    cc_linear_mxfp4_workspace_bytes, CC_NORM_NONE, CC_NORM_RMS, CC_NORM_LAYER, CC_GATE_LINEAR,
+    CC_GATE_SIGMOID,
 )

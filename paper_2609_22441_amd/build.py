@@ -15,7 +15,8 @@ LIB = PKG / "libccjoin.so"
 MARSHAL = PKG / "_marshal.so"
 SOURCES = [CSRC / "cc_api.hip", CSRC / "join_kernels.hip", CSRC / "sort_kernels.hip",
            CSRC / "part_sort_kernels.hip", CSRC / "map_kernels.hip", CSRC / "layers_api.hip",
-           CSRC / "row_kernels.hip", CSRC / "embedding_grad_kernels.hip", CSRC / "i8_kernels.hip"]
+           CSRC / "row_kernels.hip", CSRC / "embedding_grad_kernels.hip", CSRC / "i8_kernels.hip",
+           CSRC / "norm_kernels.hip", CSRC / "norm_grad_kernels.hip", CSRC / "mx_kernels.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

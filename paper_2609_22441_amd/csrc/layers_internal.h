@@ -1,5 +1,6 @@
 // Internal interface between the C ABI layer (layers_api.hip) and the kernels of the scoring
-// model's input layer (row_kernels.hip, embedding_grad_kernels.hip, i8_kernels.hip).
+// model's layers (row_kernels.hip, embedding_grad_kernels.hip, i8_kernels.hip, norm_kernels.hip,
+// norm_grad_kernels.hip, mx_kernels.hip).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -82,5 +83,64 @@ struct LinearArgs {
     float *scales;
 };
 hipError_t launch_linear(const LinearArgs &x, const ProductArgs &product, hipStream_t stream);
+
+enum Norm : int32_t { kNormNone = 0, kNormRms = 1, kNormLayer = 2 };
+enum Gate : int32_t { kGateLinear = 0, kGateSigmoid = 1, kGateNone = 2 };
+
+// n = post(f), y = x + scale * g * n, h = pre(y): x, weights, biases and h or NULL.
+struct NormArgs {
+    const void *x, *f, *gate;
+    void *y, *h;
+    const float *post_weight, *post_bias, *pre_weight, *pre_bias;
+    int64_t x_stride, f_stride, gate_stride, y_stride, h_stride;     // bytes
+    int64_t n;
+    int32_t cols, type, stream_type, post, pre, gate_kind;
+    float post_eps, pre_eps, scale;
+};
+hipError_t launch_norm(const NormArgs &a, hipStream_t stream);
+
+// Sums over rows, in this order wherever they are numbered.
+enum Sum : int { kPostWeight = 0, kPreWeight = 1, kPostBias = 2, kPreBias = 3, kSums = 4 };
+
+// The gradients, of NormArgs without y, h and pre_bias: dy, dh, dx, dgate or sums may be NULL.
+struct NormGradArgs {
+    NormArgs a;
+    const void *dy, *dh;
+    void *dx, *df, *dgate;
+    int64_t dy_stride, dh_stride, dx_stride, df_stride, dgate_stride;       // bytes
+    float *sums[kSums];
+    void *workspace;
+    bool accumulate;
+};
+int64_t norm_grad_workspace_bytes(int64_t n, int32_t cols);
+hipError_t launch_norm_grad(const NormGradArgs &a, hipStream_t stream);
+
+// Rows in microscaled 4-bit floating point.
+constexpr int32_t kMxBlock = 32;                  // values with one scale
+inline int64_t mx_padded(int64_t k) { return (k + 127) & ~(int64_t)127; }
+inline int64_t mx_scales(int64_t k) { return (k + 511) / 512 * 16; }       // bytes of a row's scales
+
+struct MxRowsArgs {
+    const void *x;                                // the rows of the other type; written by dequantise
+    uint8_t *q, *scales;
+    int64_t x_stride, q_stride, scales_stride;    // bytes
+    int64_t n;
+    int32_t cols, type;
+};
+hipError_t launch_mx_quantize(const MxRowsArgs &a, hipStream_t stream);
+hipError_t launch_mx_dequantize(const MxRowsArgs &a, hipStream_t stream);
+
+struct MxProductArgs {
+    const uint8_t *a, *b, *a_scales, *b_scales;
+    const float *bias;
+    void *out;
+    int64_t a_stride, b_stride, a_scales_stride, b_scales_stride, out_stride;   // bytes
+    int64_t m, n, k;
+    int32_t out_type;
+    bool relu;
+};
+hipError_t launch_mx_product(const MxProductArgs &a, hipStream_t stream);
+// The product of rows that are quantised on the way: product.a, a_scales: room for their 4-bit form.
+hipError_t launch_mx_linear(const MxRowsArgs &x, const MxProductArgs &product, hipStream_t stream);
 
 }  // namespace ccj

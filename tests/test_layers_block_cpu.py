@@ -1,0 +1,358 @@
+"""CPU checks of the block norms and the 4-bit rows: what the C interface and the binding refuse before
+anything touches a device, workspace sizes, and pins of the oracle that the GPU tests compare with."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+import block_oracle as O
+import layers_common as C
+from paper_2609_22441_amd import binding as B
+from paper_2609_22441_amd import layers as Y
+from test_layers_cpu import BAD, BF16, F16, NAN, Stub, At, caller, g
+
+INF = float("inf")
+U8 = torch.uint8
+
+
+# ---- the C interface ----
+
+NORM = dict(x=0x100000, x_stride=128, stream_type=0, f=0x200000, f_stride=64, gate=0x300000,
+            gate_stride=64, gate_kind=1, type=2, post=1, post_weight=0x400000, post_bias=0x410000,
+            post_eps=1e-5, pre=2, pre_weight=0x420000)
+NORM_REFUSALS = [
+    dict(n=-1), dict(n=1 << 31), dict(cols=0), dict(cols=(1 << 24) + 1), dict(type=3),
+    dict(type=-1), dict(stream_type=1), dict(stream_type=4), dict(type=0, stream_type=2),
+    dict(post=3), dict(post=-1), dict(pre=3), dict(gate_kind=2), dict(gate_kind=-1),
+    dict(post_eps=0.0), dict(post_eps=-1.0), dict(post_eps=NAN), dict(post_eps=INF),
+    dict(post_eps=1e-60), dict(post_eps=1e39), dict(pre_eps=0.0), dict(scale=NAN), dict(scale=INF),
+    dict(scale=1e39), dict(post_weight=0x400002), dict(post_bias=0x410001),
+    dict(pre_weight=0x420003), dict(x=0x100002), dict(x_stride=126), dict(x_stride=130),
+    dict(f=None), dict(f=0x200001), dict(f_stride=62), dict(f_stride=65), dict(gate=0x300001),
+    dict(gate_stride=0), dict(f_stride=1 << 62)]
+
+
+def test_norm_refuses():
+    call = caller("cc_block_norm", dict(
+        **NORM, pre_bias=0x430000, pre_eps=1e-5, scale=1.0, n=10, cols=32, y=0x500000, y_stride=128,
+        h=0x600000, h_stride=64, stream=None))
+    for kw in NORM_REFUSALS + [
+            dict(pre_bias=0x430001), dict(y=None), dict(y=0x500002), dict(y_stride=124),
+            dict(h=0x600001), dict(h_stride=62), dict(y=0x100080), dict(y=0x100000, y_stride=256),
+            dict(y=0x200000), dict(y=0x300000), dict(y=0x400000), dict(y=0x410000),
+            dict(y=0x420000), dict(y=0x430000), dict(y=0x600000), dict(h=0x100000),
+            dict(h=0x200040), dict(h=0x200000, h_stride=128), dict(h=0x300000), dict(h=0x400000),
+            dict(h=0x430000 - 2), dict(h=0x500000 + 9 * 128)]:
+        assert call(**kw) == BAD, kw
+    assert call(n=0, x=None, f=None, gate=None, y=None) == 0
+    assert call(n=0, cols=0) == BAD
+    # What a call does not use is not checked.
+    assert call(n=0, gate=None, gate_kind=7) == 0
+    assert call(n=0, h=None, pre=9, pre_eps=-1.0, pre_weight=3, pre_bias=1) == 0
+    assert call(n=0, post=0, post_eps=-1.0) == 0
+
+
+def test_norm_grad_refuses():
+    need = Y.cc_block_norm_grad_workspace_bytes(10, 32)
+    assert need > 0
+    call = caller("cc_block_norm_grad", dict(
+        **NORM, pre_eps=1e-5, scale=1.0, n=10, cols=32, dy=0x500000, dy_stride=128, dh=0x510000,
+        dh_stride=64, dx=0x520000, dx_stride=128, df=0x530000, df_stride=64, dgate=0x540000,
+        dgate_stride=64, d_post_weight=0x600000, d_post_bias=0x610000, d_pre_weight=0x620000,
+        d_pre_bias=0x630000, accumulate=0, workspace=0x700000, workspace_bytes=need, stream=None))
+    for kw in NORM_REFUSALS + [
+            dict(dy=None, dh=None), dict(dh=None), dict(gate=None), dict(df=None), dict(dy=0x500002),
+            dict(dy_stride=124), dict(dh=0x510001), dict(dh_stride=62), dict(dx=0x520001),
+            dict(dx_stride=120), dict(df=0x530001), dict(df_stride=63), dict(dgate=0x540001),
+            dict(dgate_stride=62), dict(d_post_weight=0x600002), dict(d_pre_bias=0x630001),
+            dict(workspace=None), dict(workspace=0x700008), dict(workspace_bytes=need - 1),
+            dict(dx=0x500000, dx_stride=256), dict(dx=0x500004), dict(dx=0x100000),
+            dict(dx=0x530000), dict(df=0x510002), dict(df=0x200000), dict(df=0x300000),
+            dict(dgate=0x300000), dict(dgate=0x530000), dict(dgate=0x510000),
+            dict(d_post_weight=0x400000), dict(d_post_bias=0x600000), dict(d_pre_weight=0x530000),
+            dict(d_pre_bias=0x700000), dict(workspace=0x200000), dict(workspace=0x520000)]:
+        assert call(**kw) == BAD, kw
+    nothing = dict(n=0, x=None, f=None, gate=None, dy=None, dh=None, dx=None, df=None, dgate=None,
+                   workspace=None, workspace_bytes=0, accumulate=1)
+    assert call(**nothing) == 0
+    for sizes in ((0, 8), (-1, 8), (5, 0), (5, (1 << 24) + 1), (1 << 31, 8)):
+        assert Y.cc_block_norm_grad_workspace_bytes(*sizes) == 0, sizes
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 1), (7, 97), (131_072, 96), (65_536, 4_096), (3, 16_384),
+                                       (9, 16_385), (2, 1 << 24), ((1 << 31) - 1, 16),
+                                       ((1 << 31) - 1, 1 << 24)])
+def test_norm_grad_workspace_stays_small(rows, cols):
+    """Some hundred rows of sums, and of long rows 32 bytes each."""
+    size = Y.cc_block_norm_grad_workspace_bytes(rows, cols)
+    assert 0 < size <= 32 * rows + 16 * (cols + 8) * min(rows, 1024)
+
+
+def test_mxfp4_rows_refuse():
+    base = dict(x=0x100000, x_stride=400, type=2, n=10, cols=200, q=0x200000, q_stride=128,
+                scales=0x300000, scales_stride=16, stream=None)
+    call = caller("cc_quantize_mxfp4", base)
+    bad = [dict(n=-1), dict(n=1 << 31), dict(cols=0), dict(cols=(1 << 24) + 1), dict(type=3),
+           dict(x=None), dict(q=None), dict(scales=None), dict(x=0x100001), dict(x_stride=398),
+           dict(q=0x200008), dict(q_stride=112), dict(q_stride=136), dict(scales=0x300004),
+           dict(scales_stride=12), dict(scales_stride=20), dict(scales_stride=0)]
+    for kw in bad + [dict(q=0x100000), dict(scales=0x100000), dict(scales=0x200000)]:
+        assert call(**kw) == BAD, kw
+    assert call(n=0, x=None, q=None, scales=None) == 0
+    order = ("q", "q_stride", "scales", "scales_stride", "n", "cols", "x", "x_stride", "type", "stream")
+    call = caller("cc_dequantize_mxfp4", {k: base[k] for k in order})
+    for kw in bad + [dict(x=0x200000), dict(x=0x300000 - 8)]:
+        assert call(**kw) == BAD, kw
+    assert call(n=0, x=None, q=None, scales=None) == 0
+
+
+def test_mxfp4_products_refuse():
+    call = caller("cc_matmul_mxfp4", dict(
+        a=0x100000, a_stride=320, a_scales=0x200000, a_scales_stride=32, b=0x300000, b_stride=336,
+        b_scales=0x400000, b_scales_stride=48, bias=0x500000, m=10, n=20, k=640, relu=1,
+        out=0x600000, out_stride=40, out_type=2, workspace=None, workspace_bytes=0, stream=None))
+    both = [dict(m=-1), dict(n=-1), dict(k=-128), dict(m=1 << 31), dict(n=1 << 31),
+            dict(k=(1 << 24) + 128), dict(out=None), dict(out=0x600001), dict(out_stride=38),
+            dict(out_stride=41), dict(bias=0x500002), dict(out=0x500000)]
+    for kw in both + [
+            dict(k=600), dict(k=64), dict(out_type=3), dict(a=None), dict(a_scales=None), dict(b=None),
+            dict(b_scales=None), dict(a=0x100008), dict(a_stride=304), dict(a_stride=324),
+            dict(a_scales=0x200008), dict(a_scales_stride=16), dict(a_scales_stride=40),
+            dict(b=0x300004), dict(b_stride=304), dict(b_scales=0x400001), dict(b_scales_stride=16),
+            dict(out=0x100000), dict(out=0x200000), dict(out=0x300000), dict(out=0x400000)]:
+        assert call(**kw) == BAD, kw
+    assert call(m=0, a=None, a_scales=None, out=None) == 0
+    assert call(n=0, b=None, b_scales=None, out=None) == 0
+    assert Y.cc_matmul_mxfp4_workspace_bytes(10, 20, 640) == 0
+    need = Y.cc_linear_mxfp4_workspace_bytes(10, 20, 600)
+    assert need == 10 * (320 + 32)
+    call = caller("cc_linear_mxfp4", dict(
+        x=0x100000, x_stride=1200, type=2, w=0x300000, w_stride=320, w_scales=0x400000,
+        w_scales_stride=32, bias=0x500000, m=10, n=20, k=600, relu=1, out=0x600000, out_stride=40,
+        workspace=0x700000, workspace_bytes=need, stream=None))
+    for kw in both[2:] + [
+            dict(k=0), dict(type=5), dict(x=None), dict(x=0x100001), dict(x_stride=1198), dict(w=None),
+            dict(w_scales=None), dict(w_stride=304), dict(w_scales_stride=16), dict(workspace=None),
+            dict(workspace=0x700008), dict(workspace_bytes=need - 1), dict(out=0x100000),
+            dict(out=0x700000), dict(workspace=0x100000), dict(workspace=0x300000),
+            dict(workspace=0x400000), dict(workspace=0x500000)]:
+        assert call(**kw) == BAD, kw
+    assert call(m=0, x=None, out=None) == 0
+    for sizes in ((0, 5, 5), (5, 0, 5), (5, 5, 0), (-1, 5, 5), (1 << 31, 5, 5), (5, 5, (1 << 24) + 1)):
+        assert Y.cc_linear_mxfp4_workspace_bytes(*sizes) == 0, sizes
+
+
+# ---- the binding ----
+
+@pytest.fixture
+def stub(monkeypatch):
+    s = Stub()
+    s.u8 = U8
+    monkeypatch.setattr(Y, "_layers", s)
+    return s
+
+
+def norm_args():
+    return dict(f=g(10, 24, dtype=BF16), y=g(10, 24), x=g(10, 24), gate=g(10, 24, dtype=BF16),
+                h=g(10, 24, dtype=BF16), post_weight=g(24), post_bias=g(24), pre_weight=g(24),
+                pre_bias=g(24))
+
+
+def norm_grad_args():
+    return dict(f=g(10, 24, dtype=BF16), df=g(10, 24, dtype=BF16), workspace=g(1 << 20, dtype=U8),
+                x=g(10, 24), gate=g(10, 24, dtype=BF16), dy=g(10, 24), dh=g(10, 24, dtype=BF16),
+                dx=g(10, 24), dgate=g(10, 24, dtype=BF16), post_weight=g(24), post_bias=g(24),
+                pre_weight=g(24), pre_bias=g(24), d_post_weight=g(24), d_post_bias=g(24),
+                d_pre_weight=g(24), d_pre_bias=g(24))
+
+
+def quantize_args():
+    return dict(x=g(10, 200, dtype=F16), q=g(10, 128, dtype=U8), scales=g(10, 16, dtype=U8))
+
+
+def dequantize_args():
+    return dict(q=g(10, 128, dtype=U8), scales=g(10, 16, dtype=U8), out=g(10, 200, dtype=F16))
+
+
+def matmul_args():
+    return dict(a=g(10, 320, dtype=U8), a_scales=g(10, 32, dtype=U8), b=g(20, 320, dtype=U8),
+                b_scales=g(20, 32, dtype=U8), out=g(10, 20, dtype=BF16), bias=g(20))
+
+
+def linear_args():
+    return dict(x=g(10, 600), w=g(20, 320, dtype=U8), w_scales=g(20, 32, dtype=U8), out=g(10, 20),
+                bias=g(20), workspace=g(1 << 13, dtype=U8))
+
+
+CALLS = {"cc_block_norm": norm_args, "cc_block_norm_grad": norm_grad_args,
+         "cc_quantize_mxfp4": quantize_args, "cc_dequantize_mxfp4": dequantize_args,
+         "cc_matmul_mxfp4": matmul_args, "cc_linear_mxfp4": linear_args}
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_valid_calls_reach_the_library(stub, name):
+    getattr(Y, name)(**CALLS[name](), stream=0)
+    assert [c[0] for c in stub.calls] == [name]
+
+
+REFUSALS = [
+    ("cc_block_norm", "f", torch.zeros(10, 24, dtype=BF16), ValueError, "GPU memory"),
+    ("cc_block_norm", "f", g(10, 24, dtype=torch.int32), TypeError, "float32"),
+    ("cc_block_norm", "f", g(10, 24, dtype=BF16, device=1), ValueError, "one device"),
+    ("cc_block_norm", "y", g(10, 24, dtype=F16), TypeError, "bfloat16 as f is, or float32"),
+    ("cc_block_norm", "y", g(9, 24), ValueError, "10 rows"),
+    ("cc_block_norm", "y", g(10, 23), ValueError, "24 columns"),
+    ("cc_block_norm", "x", g(10, 24, dtype=BF16), TypeError, "float32 as y is"),
+    ("cc_block_norm", "gate", g(10, 24), TypeError, "bfloat16 as f is"),
+    ("cc_block_norm", "gate", At(torch.zeros(1, 24, dtype=BF16).expand(10, 24)), ValueError, "overlap"),
+    ("cc_block_norm", "h", g(10, 24), TypeError, "bfloat16 as f is"),
+    ("cc_block_norm", "h", At(torch.zeros(24, 10, dtype=BF16).t()), ValueError, "dense"),
+    ("cc_block_norm", "post_weight", g(24, dtype=BF16), TypeError, "float32"),
+    ("cc_block_norm", "pre_bias", g(23), ValueError, "24 elements"),
+    ("cc_block_norm", "pre_weight", g(24, device=1), ValueError, "one device"),
+    ("cc_block_norm_grad", "dy", g(10, 24, dtype=F16), TypeError, "bfloat16 as f is, or float32"),
+    ("cc_block_norm_grad", "dx", g(10, 24, dtype=BF16), TypeError, "residual stream"),
+    ("cc_block_norm_grad", "dh", g(10, 24), TypeError, "bfloat16 as f is"),
+    ("cc_block_norm_grad", "dh", None, ValueError, "need dh"),
+    ("cc_block_norm_grad", "df", g(11, 24, dtype=BF16), ValueError, "10 rows"),
+    ("cc_block_norm_grad", "gate", None, ValueError, "needs the gate"),
+    ("cc_block_norm_grad", "workspace", None, ValueError, "bytes"),
+    ("cc_block_norm_grad", "workspace", g(64, dtype=U8), ValueError, "bytes"),
+    ("cc_block_norm_grad", "d_post_bias", g(20), ValueError, "24 elements"),
+    ("cc_block_norm_grad", "d_pre_weight", g(24, dtype=BF16), TypeError, "float32"),
+    ("cc_quantize_mxfp4", "q", g(10, 100, dtype=U8), ValueError, "128 columns"),
+    ("cc_quantize_mxfp4", "q", g(10, 128, dtype=torch.int8), TypeError, "uint8"),
+    ("cc_quantize_mxfp4", "q", g(9, 128, dtype=U8), ValueError, "10 rows"),
+    ("cc_quantize_mxfp4", "scales", g(10, 7, dtype=U8), ValueError, "16 columns"),
+    ("cc_quantize_mxfp4", "scales", g(11, 16, dtype=U8), ValueError, "10 rows"),
+    ("cc_dequantize_mxfp4", "out", g(10, 300), ValueError, "192 columns"),
+    ("cc_dequantize_mxfp4", "out", g(10, 200, dtype=torch.int8), TypeError, "float32"),
+    ("cc_matmul_mxfp4", "a", g(10, 300, dtype=U8), ValueError, "multiple of 64"),
+    ("cc_matmul_mxfp4", "a_scales", g(10, 16, dtype=U8), ValueError, "32 columns"),
+    ("cc_matmul_mxfp4", "b", g(20, 256, dtype=U8), ValueError, "320 columns"),
+    ("cc_matmul_mxfp4", "b_scales", g(20, 32), TypeError, "uint8"),
+    ("cc_matmul_mxfp4", "bias", g(19), ValueError, "20 elements"),
+    ("cc_matmul_mxfp4", "out", g(10, 21, dtype=BF16), ValueError, "20 columns"),
+    ("cc_linear_mxfp4", "x", g(10, 700), ValueError, "384 columns"),
+    ("cc_linear_mxfp4", "w", g(20, 320, dtype=torch.int8), TypeError, "uint8"),
+    ("cc_linear_mxfp4", "out", g(10, 20, dtype=BF16), TypeError, "float32"),
+    ("cc_linear_mxfp4", "workspace", None, ValueError, "bytes"),
+]
+
+
+@pytest.mark.parametrize("name,arg,bad,exc,match", REFUSALS)
+def test_binding_refuses(stub, name, arg, bad, exc, match):
+    a = CALLS[name]()
+    a[arg] = bad
+    with pytest.raises(exc, match=match):
+        getattr(Y, name)(**a, stream=0)
+    assert stub.calls == []
+
+
+def test_binding_refuses_a_gradient_of_nothing(stub):
+    a = norm_grad_args()
+    for name in ("dy", "dh", "d_pre_weight", "d_pre_bias"):
+        a[name] = None
+    with pytest.raises(ValueError, match="one of them"):
+        Y.cc_block_norm_grad(**a, stream=0)
+    assert stub.calls == []
+
+
+def test_other_norms_raise():
+    a = {k: v for k, v in norm_args().items()}
+    with pytest.raises(ValueError, match="GPU memory"):
+        Y.cc_block_norm(**{k: v.t for k, v in a.items()}, stream=0)
+
+
+# ---- pins of the oracle ----
+
+def torch_norm(c, leaves):
+    """The call in torch's 64 bits, for its automatic gradient."""
+    def unit(v, kind, eps):
+        if kind == O.NONE:
+            return v
+        if kind == O.LAYER:
+            return torch.nn.functional.layer_norm(v, v.shape[-1:], eps=float(np.float32(eps)))
+        return torch.nn.functional.rms_norm(v, v.shape[-1:], eps=float(np.float32(eps)))
+
+    n = unit(leaves["f"], c["post_norm"], c["post_eps"])
+    n = n * leaves["post_weight"] + leaves["post_bias"]
+    g_ = torch.sigmoid(leaves["gate"]) if c["gate_kind"] == O.SIGMOID else leaves["gate"]
+    y = leaves["x"] + float(np.float32(c["scale"])) * g_ * n
+    return y, unit(y, c["pre_norm"], c["pre_eps"]) * leaves["pre_weight"] + leaves["pre_bias"]
+
+
+@pytest.mark.parametrize("post", [O.NONE, O.RMS, O.LAYER])
+@pytest.mark.parametrize("pre", [O.NONE, O.RMS, O.LAYER])
+@pytest.mark.parametrize("gate_kind", [O.LINEAR, O.SIGMOID])
+def test_oracle_is_the_automatic_gradient(post, pre, gate_kind):
+    r = np.random.default_rng(post * 9 + pre * 3 + gate_kind)
+    c = dict(post_norm=post, pre_norm=pre, gate_kind=gate_kind, scale=0.3, post_eps=1e-3, pre_eps=2e-3)
+    for name, shape in (("f", (6, 20)), ("x", (6, 20)), ("gate", (6, 20)), ("post_weight", 20),
+                        ("post_bias", 20), ("pre_weight", 20), ("pre_bias", 20)):
+        c[name] = r.standard_normal(shape)
+    leaves = {k: torch.tensor(c[k], requires_grad=True) for k in c if isinstance(c[k], np.ndarray)}
+    y, h = torch_norm(c, leaves)
+    got = O.norm(c)
+    assert np.allclose(got[0].v, y.detach().numpy()) and np.allclose(got[1].v, h.detach().numpy())
+    dy, dh = r.standard_normal((6, 20)), r.standard_normal((6, 20))
+    ((y * torch.tensor(dy)).sum() + (h * torch.tensor(dh)).sum()).backward()
+    got = O.norm_grad(c, dy, dh)
+    for k, leaf in (("df", "f"), ("dx", "x"), ("dgate", "gate"), ("d_post_weight", "post_weight"),
+                    ("d_post_bias", "post_bias"), ("d_pre_weight", "pre_weight"),
+                    ("d_pre_bias", "pre_bias")):
+        assert np.allclose(got[k].v.reshape(c[leaf].shape), leaves[leaf].grad.numpy()), k
+
+
+def test_bounds_hold_for_32_bits_and_are_tight():
+    """NumPy's float32 run of the formulas stays within the bounds, which are below 200 roundings of the
+    largest output."""
+    r = np.random.default_rng(4)
+    for post, pre in ((O.RMS, O.LAYER), (O.LAYER, O.RMS)):
+        c = dict(post_norm=post, pre_norm=pre, gate_kind=O.LINEAR, scale=0.5, post_eps=1e-5, pre_eps=1e-5)
+        for name, shape in (("f", (50, 300)), ("x", (50, 300)), ("gate", (50, 300))):
+            c[name] = r.standard_normal(shape).astype(np.float32).astype(np.float64)
+
+        def unit(v, kind):
+            if kind == O.LAYER:
+                v = v - v.mean(1, keepdims=True)
+            return v / np.sqrt((v * v).mean(1, keepdims=True) + np.float32(1e-5))
+
+        f, x, u = (c[k].astype(np.float32) for k in ("f", "x", "gate"))
+        y = x + np.float32(0.5) * u * unit(f, post)
+        h = unit(y, pre)
+        assert y.dtype == h.dtype == np.float32
+        for got, want in ((y, O.norm(c)[0]), (h, O.norm(c)[1])):
+            assert (np.abs(got - want.v) <= want.e).all()
+            assert want.e.max() <= 200 * C.F32 * np.abs(want.v).max()
+
+
+def test_quantisation_picks_the_nearest_value():
+    """Of every code, no other is nearer; the largest of a block lies from 3.5 to 7 scales; halves of the
+    grid's distance bound the errors."""
+    r = np.random.default_rng(6)
+    x = (r.standard_normal((40, 70)) * 2.0 ** r.integers(-30, 30, (40, 1))).astype(np.float32)
+    codes, scales = O.quantize(x.astype(np.float64))
+    assert codes.shape == (40, 128) and scales.shape == (40, 16)
+    assert (codes[:, 70:] == 0).all() and (scales[:, 3:] == 0).all()
+    got = O.values(codes, scales)[:, :70]
+    unit = np.repeat(2.0 ** (scales[:, :3].astype(float) - 127), 32, axis=1)[:, :70]
+    for b in range(3):
+        most = np.abs(x[:, b * 32:(b + 1) * 32]).max(1) / unit[:, b * 32]
+        assert (most >= 3.5).all() and (most < 7).all()
+    a = np.abs(x) / unit
+    half = np.select([a < 2, a < 4], [0.25, 0.5], 1.0)
+    assert (np.abs(got - x) <= half * unit * (1 + 1e-12)).all()
+
+
+def test_quantisation_by_hand():
+    x = np.zeros((1, 64))
+    x[0, :12] = [4.0, 5.0, -5.5, 0.25, 0.75, -1.25, 1.75, 2.5, 3.5, 6.9, -0.1, 0.26]
+    x[0, 32:35] = [7.0, 1.0, -3.0]                # rounds up to 8: scales of 2
+    codes, scales = O.quantize(x)
+    assert list(scales[0, :2]) == [127, 128]
+    assert list(codes[0, :12]) == [6, 6, 15, 0, 2, 10, 4, 4, 6, 7, 8, 1]
+    assert list(codes[0, 32:35]) == [6, 1, 8 | 3]
+    assert O.packed(codes)[0, 0] == 0x66
+    assert list(O.values(codes, scales)[0, 32:35]) == [8.0, 1.0, -3.0]

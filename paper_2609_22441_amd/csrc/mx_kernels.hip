@@ -1,5 +1,8 @@
 // Rows in microscaled 4-bit floating point: to 4 bits, back, and the product of two such matrices.
+#include <type_traits>
+
 #include "layers_device.h"
+#include "mx_choice.h"
 
 namespace ccj {
 namespace {
@@ -222,6 +225,296 @@ __device__ __forceinline__ float4_t multiply16(int4_t a, int4_t b, float4_t c, i
                                                             scale_a, BYTE, scale_b);
 }
 
+typedef float float16_tile __attribute__((ext_vector_type(16)));
+typedef __attribute__((address_space(1))) const void global_void;
+typedef __attribute__((address_space(3))) void lds_void;
+
+// The same over 64 of k, of 32 rows each: lane l holds the values of row l % 32 in block l / 32.
+template <int BYTE>
+__device__ __forceinline__ float16_tile multiply32(int4_t a, int4_t b, float16_tile c, int scale_a,
+                                                   int scale_b) {
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(a), operand(b), c, 4, 4, BYTE,
+                                                           scale_a, BYTE, scale_b);
+}
+
+__device__ const int4_t kZeros = {0, 0, 0, 0};    // read in the place of columns past k
+
+constexpr int kStep = 64;                         // bytes of k per stage: 128 values, 4 scales
+constexpr int kGroup = 4;                         // stages whose scales are fetched together
+
+// s_waitcnt's operand for at most `vm` vector loads outstanding and no LDS operation.
+constexpr int wait_loads(int vm) { return (vm & 15) | (vm >> 4) << 14 | 7 << 4; }
+
+// The order of memory accesses around a barrier is the source's.
+__device__ __forceinline__ void stage_barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Where 16-byte chunk c (0 to 3) of row r lies among the four of the row's 64 bytes: any 8 or 16
+// consecutive rows have the chunks of one c in different banks.
+__device__ __forceinline__ int swizzled(int row, int chunk) {
+    return chunk ^ (((row >> 2) & 1) << 1 | (((row >> 1) ^ (row >> 3)) & 1));
+}
+
+// Tiles of TM rows of a by TN of b, WM x WN wavefronts. Stages of 64 bytes of k go from memory to LDS
+// without passing through registers, kStages - 1 ahead of the one that is multiplied; the scales of
+// four stages go with the first of them, 16 bytes a row, as a fetch of 4 bytes a row would keep the
+// address unit as long as the rows' values do. The weights are the first operand, so that a lane holds
+// four consecutive columns of one output row; the results pass through LDS once more, to be written in
+// whole rows of the wavefront's columns.
+//
+// SPLIT groups of WM x WN wavefronts take every SPLIT-th four stages of k each, for tiles too few to
+// fill the chip; their sums meet in LDS, in the groups' order.
+template <typename TO, int TM, int TN, int WM, int WN, int SPLIT, int kStages>
+__global__ __launch_bounds__(64 * WM * WN * SPLIT, 2) void tile_kernel(MxProductArgs p,
+                                                                       uint32_t tiles_m,
+                                                                       uint32_t tiles_n) {
+    constexpr int kWaves = WM * WN, kT = 64 * kWaves;            // of a group
+    constexpr int kMB = TM / WM / 32, kNB = TN / WN / 32;        // 32 x 32 blocks of a wavefront
+    constexpr int kLoadsA = TM * kStep / 16 / kT, kLoadsB = TN * kStep / 16 / kT;
+    constexpr int kLoads = kLoadsA + kLoadsB;
+    constexpr int kStageBytes = (TM + TN) * kStep;
+    // Rows of scales are fetched in kScaleLoads rounds by the wavefronts that they suffice for, to two
+    // places: the one of four stages is written again only after the next four have begun.
+    constexpr int kScaleRows = TM + TN, kScaleLoads = (kScaleRows + kT - 1) / kT;
+    constexpr int kScaleBytes = kScaleRows * 16;
+    static_assert(kScaleRows % 64 == 0, "");
+    // A wavefront's results of 32 rows, 16 bytes more per row against bank conflicts.
+    constexpr int kPitch = kNB * 32 * sizeof(TO) + 16;
+    static_assert(kStages >= 3 && kStages <= kGroup && kLoadsA >= 1 && kLoadsB >= 1, "");
+    constexpr int kGroupBytes = kStages * kStageBytes + 2 * kScaleBytes;
+    constexpr int kSums = kWaves * kMB * kNB * 4096;             // bytes of a group's sums
+    static_assert(SPLIT == 1 || kSums <= kGroupBytes, "");
+    constexpr int kStaged = SPLIT * kGroupBytes, kOutput = 32 * kPitch * kWaves;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[kStaged > kOutput ? kStaged : kOutput];
+    __shared__ __attribute__((aligned(16))) float bias[TN];
+
+    // Workgroups go round the 8 XCDs; each gets consecutive tiles, in groups of 4 rows of tiles, so
+    // that those it works on together share their rows of a and b in its L2.
+    uint32_t id = blockIdx.x;
+    {
+        const uint32_t total = tiles_m * tiles_n, share = total / 8, more = total % 8;
+        const uint32_t xcd = id % 8;
+        id = xcd * share + min(xcd, more) + id / 8;
+    }
+    const uint32_t group = id / (4 * tiles_n), rows = min(4u, tiles_m - group * 4);
+    const uint32_t in = id - group * 4 * tiles_n;
+    const int64_t m0 = (int64_t)(group * 4 + in % rows) * TM, n0 = (int64_t)(in / rows) * TN;
+
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % kWaves;
+    const int split = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / kWaves;
+    const int wm = wave / WN, wn = wave % WN;
+    // Thread t of a group moves 16 bytes of row t / 4 (and every kT / 4 rows on) to LDS byte 16 t, and
+    // 16 scales of row t (and every kT rows on).
+    const int thread = threadIdx.x % kT, row = thread >> 2, chunk = swizzled(row & 15, thread & 3);
+    const uint8_t *from[kLoads], *scales[kScaleLoads];
+#pragma unroll
+    for (int i = 0; i < kLoadsA; ++i)             // rows past the last repeat it: not written
+        from[i] = p.a + min(m0 + row + i * (kT / 4), p.m - 1) * p.a_stride + chunk * 16;
+#pragma unroll
+    for (int i = 0; i < kLoadsB; ++i)
+        from[kLoadsA + i] = p.b + min(n0 + row + i * (kT / 4), p.n - 1) * p.b_stride + chunk * 16;
+#pragma unroll
+    for (int i = 0; i < kScaleLoads; ++i) {
+        const int at = thread + i * kT;           // rows of a, then of b; past them any row
+        scales[i] = at < TM ? p.a_scales + min(m0 + at, p.m - 1) * p.a_scales_stride
+                            : p.b_scales + min(n0 + at - TM, p.n - 1) * p.b_scales_stride;
+    }
+    for (int i = threadIdx.x; i < TN; i += kT * SPLIT)
+        bias[i] = p.bias ? p.bias[min(n0 + i, p.n - 1)] : 0.0f;
+    // Stages of k, and how many of them are this group's.
+    const int all = (int)(p.k / 2 / kStep);
+    const int fours = all / kGroup, rest = all % kGroup;
+    const int steps = SPLIT == 1 ? all
+                                 : ((fours + SPLIT - 1 - split) / SPLIT) * kGroup +
+                                       (fours % SPLIT == split ? rest : 0);
+    uint8_t *const stages = lds + split * kGroupBytes;
+    uint8_t *const scale_places = stages + kStages * kStageBytes;
+    auto fetch = [&](int step) {
+        const int four = step / kGroup * SPLIT + split;          // number of its four stages in k
+        if (step % kGroup == 0) {
+            uint8_t *to = scale_places + step / kGroup % 2 * kScaleBytes + wave * 1024;
+#pragma unroll
+            for (int i = 0; i < kScaleLoads; ++i)
+                if (wave * 64 + i * kT < kScaleRows)
+                    __builtin_amdgcn_global_load_lds((global_void *)(scales[i] + four * 16),
+                                                     (lds_void *)(to + i * kT * 16), 16, 0, 0);
+        }
+        uint8_t *to = stages + wave * 1024 + step % kStages * kStageBytes;
+        const int64_t at = (int64_t)(four * kGroup + step % kGroup) * kStep;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int place = i < kLoadsA ? i * kT * 16 : TM * kStep + (i - kLoadsA) * kT * 16;
+            __builtin_amdgcn_global_load_lds((global_void *)(from[i] + at), (lds_void *)(to + place),
+                                             16, 0, 0);
+        }
+    };
+    float16_tile acc[kMB][kNB] = {};
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s)
+        if (s < steps)
+            fetch(s);
+    // A fragment: lane l holds 16 bytes of row l % 32, of a stage's four chunks number 2 (l / 32) first,
+    // then the one after it: the sum over k may take them in any order, and so the scales of a lane are
+    // two neighbours of the stage's four.
+    const int frow = lane & 31, upper = lane >> 5;
+    const uint8_t *const sa = stages + (wm * (TM / WM) + frow) * kStep;
+    const uint8_t *const sb = stages + (TM + wn * (TN / WN) + frow) * kStep;
+    const uint8_t *const ca = scale_places + (wm * (TM / WM) + frow) * 16;
+    const uint8_t *const cb = scale_places + (TM + wn * (TN / WN) + frow) * 16;
+    const int at[2] = {swizzled(frow & 15, upper * 2) * 16, swizzled(frow & 15, upper * 2 + 1) * 16};
+    int4_t fa[2][kMB], fb[2][kNB];                // of both halves of a stage
+    int ea[kMB], eb[kNB], next_a[kMB], next_b[kNB];       // scales of a stage and of the next
+    auto read = [&](int h, int step) {
+        const int stage = step % kStages * kStageBytes;
+#pragma unroll
+        for (int j = 0; j < kNB; ++j)
+            fb[h][j] = *(const int4_t *)(sb + stage + j * 32 * kStep + at[h]);
+#pragma unroll
+        for (int i = 0; i < kMB; ++i)
+            fa[h][i] = *(const int4_t *)(sa + stage + i * 32 * kStep + at[h]);
+    };
+    auto read_scales = [&](int step) {
+        const int place = step / kGroup % 2 * kScaleBytes + step % kGroup * 4 + upper * 2;
+#pragma unroll
+        for (int j = 0; j < kNB; ++j)
+            next_b[j] = *(const uint16_t *)(cb + place + j * 32 * 16);
+#pragma unroll
+        for (int i = 0; i < kMB; ++i)
+            next_a[i] = *(const uint16_t *)(ca + place + i * 32 * 16);
+    };
+    auto multiply = [&](auto half) {
+        constexpr int h = decltype(half)::value;
+#pragma unroll
+        for (int i = 0; i < kMB; ++i)
+#pragma unroll
+            for (int j = 0; j < kNB; ++j)
+                acc[i][j] = multiply32<h>(fb[h][j], fa[h][i], acc[i][j], eb[j], ea[i]);
+        // One read after each of the first matrix instructions, so that none of them waits for it.
+#pragma unroll
+        for (int i = 0; i < 2 * (kMB + kNB) && i < kMB * kNB; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto take_scales = [&] {
+#pragma unroll
+        for (int j = 0; j < kNB; ++j)
+            eb[j] = next_b[j];
+#pragma unroll
+        for (int i = 0; i < kMB; ++i)
+            ea[i] = next_a[i];
+    };
+    // Loads of the scales come on top of what is waited for at least: then a wait is for more than it
+    // needs.
+    if (steps >= kStages - 1)
+        __builtin_amdgcn_s_waitcnt(wait_loads((kStages - 2) * kLoads));
+    else
+        __builtin_amdgcn_s_waitcnt(wait_loads(0));
+    stage_barrier();
+    // The fragments that one half's matrix instructions take are read while the other half's run; so
+    // a step begins with its first half in registers and reads into the next stage at its end.
+    read(0, 0);
+    read_scales(0);
+    take_scales();
+    const int most = SPLIT == 1 ? steps         // of any group
+                                : (fours + SPLIT - 1) / SPLIT * kGroup + (fours % SPLIT ? 0 : rest);
+    for (int step = 0; step < most; ++step) {
+        if (step + kStages - 2 < steps)
+            __builtin_amdgcn_s_waitcnt(wait_loads((kStages - 3) * kLoads));
+        else
+            __builtin_amdgcn_s_waitcnt(wait_loads(0));
+        // Every wavefront's loads of the next stage are in LDS, and the stage whose place is
+        // fetched into has been read by all.
+        stage_barrier();
+        if (SPLIT > 1 && step >= steps)           // others of the workgroup go on
+            continue;
+        __builtin_amdgcn_sched_barrier(0);
+        read(1, step);
+        multiply(std::integral_constant<int, 0>());
+        if (step + kStages - 1 < steps)
+            fetch(step + kStages - 1);
+        __builtin_amdgcn_sched_barrier(0);
+        read(0, step + 1);                        // past the last step: not used
+        read_scales(step + 1);
+        multiply(std::integral_constant<int, 1>());
+        take_scales();
+    }
+    stage_barrier();                              // the stages' LDS now holds results
+    if constexpr (SPLIT > 1) {
+        if (split)
+#pragma unroll
+            for (int b = 0; b < kMB * kNB; ++b)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    *(float4_t *)(stages + ((wave * kMB * kNB + b) * 4 + g) * 1024 + lane * 16) =
+                        float4_t{acc[b / kNB][b % kNB][4 * g], acc[b / kNB][b % kNB][4 * g + 1],
+                                 acc[b / kNB][b % kNB][4 * g + 2], acc[b / kNB][b % kNB][4 * g + 3]};
+        __syncthreads();
+        if (split)
+            return;
+#pragma unroll
+        for (int s = 1; s < SPLIT; ++s)
+#pragma unroll
+            for (int b = 0; b < kMB * kNB; ++b)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const float4_t v = *(const float4_t *)(stages + s * kGroupBytes +
+                                                           ((wave * kMB * kNB + b) * 4 + g) * 1024 +
+                                                           lane * 16);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        acc[b / kNB][b % kNB][4 * g + r] += v[r];
+                }
+    }
+
+    uint8_t *mine = lds + wave * 32 * kPitch;
+    const int64_t wave_m = m0 + wm * (TM / WM), wave_n = n0 + wn * (TN / WN);
+    constexpr int kEach = 16 / sizeof(TO), kLanes = kNB * 32 / kEach;       // lanes per output row
+#pragma unroll
+    for (int i = 0; i < kMB; ++i) {
+#pragma unroll
+        for (int j = 0; j < kNB; ++j)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                // Registers 4 g to 4 g + 3: columns 8 g + 4 (lane / 32) and the three after it.
+                const int col = j * 32 + g * 8 + upper * 4;
+                typedef TO out4_t __attribute__((ext_vector_type(4)));
+                float4_t y;
+                const float4_t bb = *(const float4_t *)(bias + wn * (TN / WN) + col);
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    y[r] = finish(acc[i][j][g * 4 + r], bb[r], p.relu);
+                *(out4_t *)(mine + frow * kPitch + col * sizeof(TO)) =
+                    __builtin_convertvector(y, out4_t);
+            }
+        // The wavefront's own rows: its LDS writes come before its reads.
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int r = 0; r < 32; r += 64 / kLanes) {
+            const int at_row = r + lane / kLanes, col = lane % kLanes * kEach;
+            const int64_t to_m = wave_m + i * 32 + at_row, n = wave_n + col;
+            if (to_m < p.m && n < p.n) {
+                const words_t w = (words_t) * (const int4_t *)(mine + at_row * kPitch + col * sizeof(TO));
+                TO *out = (TO *)((char *)p.out + to_m * p.out_stride) + n;
+                if (n + kEach <= p.n) {
+                    __builtin_nontemporal_store(w, (words_t *)out);
+                } else {
+                    TO v[kEach];
+                    __builtin_memcpy(v, &w, 16);
+                    for (int e = 0; n + e < p.n; ++e)
+                        out[e] = v[e];
+                }
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+}
+
 constexpr int kSkinnyWaves = 8;
 
 // A workgroup has 16 x 16 results and its 8 wavefronts share out k, in slabs of 512 values; fragments
@@ -278,6 +571,16 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void skinny_kernel(MxProductArgs
     }
 }
 
+template <typename TO, int TM, int TN, int WM, int WN, int SPLIT, int STAGES = 4>
+hipError_t launch_tiles(const MxProductArgs &p, hipStream_t stream) {
+    const int64_t tm = (p.m + TM - 1) / TM, tn = (p.n + TN - 1) / TN;
+    if (tm * tn * (64 * WM * WN * SPLIT) > (int64_t)UINT32_MAX)
+        return hipErrorInvalidConfiguration;
+    tile_kernel<TO, TM, TN, WM, WN, SPLIT, STAGES>
+        <<<(unsigned)(tm * tn), 64 * WM * WN * SPLIT, 0, stream>>>(p, (uint32_t)tm, (uint32_t)tn);
+    return hipGetLastError();
+}
+
 template <typename TO>
 hipError_t launch_skinny(const MxProductArgs &p, hipStream_t stream) {
     const int64_t tiles = (p.m + 15) / 16 * ((p.n + 15) / 16);
@@ -285,6 +588,18 @@ hipError_t launch_skinny(const MxProductArgs &p, hipStream_t stream) {
         return hipErrorInvalidConfiguration;
     skinny_kernel<TO><<<(unsigned)tiles, 64 * kSkinnyWaves, 0, stream>>>(p);
     return hipGetLastError();
+}
+
+template <typename TO>
+hipError_t launch_product_type(const MxProductArgs &p, hipStream_t stream) {
+    switch (mx_product_choice(p.m, p.n, p.k)) {
+    case kMxSkinny: return launch_skinny<TO>(p, stream);
+    case kMxTile64: return launch_tiles<TO, 64, 64, 2, 2, 4>(p, stream);
+    case kMxTile128x64: return launch_tiles<TO, 128, 64, 2, 2, 2>(p, stream);
+    case kMxTile128Split: return launch_tiles<TO, 128, 128, 2, 2, 2>(p, stream);
+    case kMxTile128: return launch_tiles<TO, 128, 128, 2, 2, 1>(p, stream);
+    default: return launch_tiles<TO, 256, 256, 2, 4, 1>(p, stream);
+    }
 }
 
 }  // namespace
@@ -307,9 +622,9 @@ hipError_t launch_mx_dequantize(const MxRowsArgs &a, hipStream_t stream) {
 
 hipError_t launch_mx_product(const MxProductArgs &p, hipStream_t stream) {
     switch (p.out_type) {
-    case kF32: return launch_skinny<float>(p, stream);
-    case kF16: return launch_skinny<half_t>(p, stream);
-    default: return launch_skinny<bf16_t>(p, stream);
+    case kF32: return launch_product_type<float>(p, stream);
+    case kF16: return launch_product_type<half_t>(p, stream);
+    default: return launch_product_type<bf16_t>(p, stream);
     }
 }
 

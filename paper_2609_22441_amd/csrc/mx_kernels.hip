@@ -226,7 +226,6 @@ __device__ __forceinline__ float4_t multiply16(int4_t a, int4_t b, float4_t c, i
 }
 
 typedef float float16_tile __attribute__((ext_vector_type(16)));
-typedef __attribute__((address_space(1))) const void global_void;
 typedef __attribute__((address_space(3))) void lds_void;
 
 // The same over 64 of k, of 32 rows each: lane l holds the values of row l % 32 in block l / 32.
@@ -237,10 +236,24 @@ __device__ __forceinline__ float16_tile multiply32(int4_t a, int4_t b, float16_t
                                                            scale_a, BYTE, scale_b);
 }
 
-__device__ const int4_t kZeros = {0, 0, 0, 0};    // read in the place of columns past k
+constexpr int kStep = 128;                        // bytes of k per stage: 256 values, 8 scales
 
-constexpr int kStep = 64;                         // bytes of k per stage: 128 values, 4 scales
-constexpr int kGroup = 4;                         // stages whose scales are fetched together
+// Rows of a matrix from one on: offsets into them are 32 bits, and nothing behind them is read whatever
+// the offset.
+constexpr int64_t kMaxStride = 1 << 24;           // 255 rows of it and one more: below 2^32
+
+struct Rows {
+    const uint8_t *p;
+    uint32_t bytes;
+    __device__ Rows(const uint8_t *matrix, int64_t stride, int64_t first, int rows, int width)
+        : p(matrix + first * stride), bytes((uint32_t)((rows - 1) * stride + width)) {}
+    // 16 bytes a lane to LDS, in the order of the lanes.
+    __device__ __forceinline__ void to_lds(uint8_t *lds, uint32_t at, int more) const {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+            __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p), 0, (int)bytes, 0x20000),
+            (lds_void *)lds, 16, at, more, 0, 0);
+    }
+};
 
 // s_waitcnt's operand for at most `vm` vector loads outstanding and no LDS operation.
 constexpr int wait_loads(int vm) { return (vm & 15) | (vm >> 4) << 14 | 7 << 4; }
@@ -252,39 +265,34 @@ __device__ __forceinline__ void stage_barrier() {
     asm volatile("" ::: "memory");
 }
 
-// Where 16-byte chunk c (0 to 3) of row r lies among the four of the row's 64 bytes: any 8 or 16
+// Where 16-byte chunk c (0 to 7) of row r lies among the eight of the row's 128 bytes: any 16
 // consecutive rows have the chunks of one c in different banks.
-__device__ __forceinline__ int swizzled(int row, int chunk) {
-    return chunk ^ (((row >> 2) & 1) << 1 | (((row >> 1) ^ (row >> 3)) & 1));
-}
+__device__ __forceinline__ int swizzled(int row, int chunk) { return chunk ^ ((row >> 1) & 7); }
 
-// Tiles of TM rows of a by TN of b, WM x WN wavefronts. Stages of 64 bytes of k go from memory to LDS
-// without passing through registers, kStages - 1 ahead of the one that is multiplied; the scales of
-// four stages go with the first of them, 16 bytes a row, as a fetch of 4 bytes a row would keep the
-// address unit as long as the rows' values do. The weights are the first operand, so that a lane holds
-// four consecutive columns of one output row; the results pass through LDS once more, to be written in
-// whole rows of the wavefront's columns.
+// Tiles of TM rows of a by TN of b, WM x WN wavefronts. A stage of k is 128 bytes of every row, a whole
+// cache line: half of one at a time would be fetched twice from L2, the caches next to the unit hold
+// less than the stages on the way. It goes from memory to LDS without passing through registers, while
+// the stage before it is multiplied; the scales of two stages go with the first of them, 16 bytes a
+// row. The weights are the first operand, so that a lane holds four consecutive columns of one output
+// row; the results pass through LDS once more, to be written in whole rows of the wavefront's columns.
 //
-// SPLIT groups of WM x WN wavefronts take every SPLIT-th four stages of k each, for tiles too few to
-// fill the chip; their sums meet in LDS, in the groups' order.
-template <typename TO, int TM, int TN, int WM, int WN, int SPLIT, int kStages>
-__global__ __launch_bounds__(64 * WM * WN * SPLIT, 2) void tile_kernel(MxProductArgs p,
-                                                                       uint32_t tiles_m,
-                                                                       uint32_t tiles_n) {
+// SPLIT groups of WM x WN wavefronts take every SPLIT-th stage of k each, for tiles too few to fill the
+// chip; their sums meet in LDS, in the groups' order.
+template <typename TO, int TM, int TN, int WM, int WN, int SPLIT>
+__global__ __launch_bounds__(64 * WM * WN * SPLIT, TM * TN / (WM * WN) > 8192 ? 1 : 2) void tile_kernel(
+    MxProductArgs p, uint32_t tiles_m, uint32_t tiles_n) {
     constexpr int kWaves = WM * WN, kT = 64 * kWaves;            // of a group
     constexpr int kMB = TM / WM / 32, kNB = TN / WN / 32;        // 32 x 32 blocks of a wavefront
     constexpr int kLoadsA = TM * kStep / 16 / kT, kLoadsB = TN * kStep / 16 / kT;
     constexpr int kLoads = kLoadsA + kLoadsB;
     constexpr int kStageBytes = (TM + TN) * kStep;
-    // Rows of scales are fetched in kScaleLoads rounds by the wavefronts that they suffice for, to two
-    // places: the one of four stages is written again only after the next four have begun.
+    // Rows of scales are fetched in kScaleLoads rounds by the wavefronts that they suffice for.
     constexpr int kScaleRows = TM + TN, kScaleLoads = (kScaleRows + kT - 1) / kT;
     constexpr int kScaleBytes = kScaleRows * 16;
-    static_assert(kScaleRows % 64 == 0, "");
+    static_assert(kScaleRows % 64 == 0 && kLoadsA >= 1 && kLoadsB >= 1, "");
     // A wavefront's results of 32 rows, 16 bytes more per row against bank conflicts.
     constexpr int kPitch = kNB * 32 * sizeof(TO) + 16;
-    static_assert(kStages >= 3 && kStages <= kGroup && kLoadsA >= 1 && kLoadsB >= 1, "");
-    constexpr int kGroupBytes = kStages * kStageBytes + 2 * kScaleBytes;
+    constexpr int kGroupBytes = 2 * (kStageBytes + kScaleBytes);
     constexpr int kSums = kWaves * kMB * kNB * 4096;             // bytes of a group's sums
     static_assert(SPLIT == 1 || kSums <= kGroupBytes, "");
     constexpr int kStaged = SPLIT * kGroupBytes, kOutput = 32 * kPitch * kWaves;
@@ -307,142 +315,153 @@ __global__ __launch_bounds__(64 * WM * WN * SPLIT, 2) void tile_kernel(MxProduct
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % kWaves;
     const int split = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / kWaves;
     const int wm = wave / WN, wn = wave % WN;
-    // Thread t of a group moves 16 bytes of row t / 4 (and every kT / 4 rows on) to LDS byte 16 t, and
+    // Thread t of a group moves 16 bytes of row t / 8 (and every kT / 8 rows on) to LDS byte 16 t, and
     // 16 scales of row t (and every kT rows on).
-    const int thread = threadIdx.x % kT, row = thread >> 2, chunk = swizzled(row & 15, thread & 3);
-    const uint8_t *from[kLoads], *scales[kScaleLoads];
+    const int thread = threadIdx.x % kT, row = thread >> 3, chunk = swizzled(row & 15, thread & 7);
+    const int bytes = (int)(p.k / 2), scale_width = (bytes + 255) / 256 * 16;
+    const int rows_a = (int)min(p.m - m0, (int64_t)TM), rows_b = (int)min(p.n - n0, (int64_t)TN);
+    const Rows a(p.a, p.a_stride, m0, rows_a, bytes), b(p.b, p.b_stride, n0, rows_b, bytes);
+    const Rows a_scales(p.a_scales, p.a_scales_stride, m0, rows_a, scale_width);
+    const Rows b_scales(p.b_scales, p.b_scales_stride, n0, rows_b, scale_width);
+    uint32_t from[kLoads], from_scales[kScaleLoads];
 #pragma unroll
     for (int i = 0; i < kLoadsA; ++i)             // rows past the last repeat it: not written
-        from[i] = p.a + min(m0 + row + i * (kT / 4), p.m - 1) * p.a_stride + chunk * 16;
+        from[i] = (uint32_t)min(row + i * (kT / 8), rows_a - 1) * (uint32_t)p.a_stride + chunk * 16;
 #pragma unroll
     for (int i = 0; i < kLoadsB; ++i)
-        from[kLoadsA + i] = p.b + min(n0 + row + i * (kT / 4), p.n - 1) * p.b_stride + chunk * 16;
+        from[kLoadsA + i] =
+            (uint32_t)min(row + i * (kT / 8), rows_b - 1) * (uint32_t)p.b_stride + chunk * 16;
 #pragma unroll
     for (int i = 0; i < kScaleLoads; ++i) {
-        const int at = thread + i * kT;           // rows of a, then of b; past them any row
-        scales[i] = at < TM ? p.a_scales + min(m0 + at, p.m - 1) * p.a_scales_stride
-                            : p.b_scales + min(n0 + at - TM, p.n - 1) * p.b_scales_stride;
+        const int at = thread + i * kT;           // rows of a, then of b; past them the last
+        from_scales[i] = at < TM ? (uint32_t)min(at, rows_a - 1) * (uint32_t)p.a_scales_stride
+                                 : (uint32_t)min(at - TM, rows_b - 1) * (uint32_t)p.b_scales_stride;
     }
     for (int i = threadIdx.x; i < TN; i += kT * SPLIT)
         bias[i] = p.bias ? p.bias[min(n0 + i, p.n - 1)] : 0.0f;
-    // Stages of k, and how many of them are this group's.
-    const int all = (int)(p.k / 2 / kStep);
-    const int fours = all / kGroup, rest = all % kGroup;
-    const int steps = SPLIT == 1 ? all
-                                 : ((fours + SPLIT - 1 - split) / SPLIT) * kGroup +
-                                       (fours % SPLIT == split ? rest : 0);
+    // Stages of k, the last perhaps half of one; how many of them are this group's, and a group's most.
+    const int all = (bytes + kStep - 1) / kStep;
+    const int steps = (all + SPLIT - 1 - split) / SPLIT, most = (all + SPLIT - 1) / SPLIT;
     uint8_t *const stages = lds + split * kGroupBytes;
-    uint8_t *const scale_places = stages + kStages * kStageBytes;
+    uint8_t *const scale_places = stages + 2 * kStageBytes;
     auto fetch = [&](int step) {
-        const int four = step / kGroup * SPLIT + split;          // number of its four stages in k
-        if (step % kGroup == 0) {
-            uint8_t *to = scale_places + step / kGroup % 2 * kScaleBytes + wave * 1024;
+        const int stage = step * SPLIT + split;
+        if (SPLIT > 1 || step % 2 == 0) {
+            uint8_t *to = scale_places + (SPLIT > 1 ? step : step / 2) % 2 * kScaleBytes + wave * 1024;
 #pragma unroll
             for (int i = 0; i < kScaleLoads; ++i)
                 if (wave * 64 + i * kT < kScaleRows)
-                    __builtin_amdgcn_global_load_lds((global_void *)(scales[i] + four * 16),
-                                                     (lds_void *)(to + i * kT * 16), 16, 0, 0);
+                    (wave * 64 + i * kT < TM ? a_scales : b_scales)
+                        .to_lds(to + i * kT * 16, from_scales[i], stage / 2 * 16);
         }
-        uint8_t *to = stages + wave * 1024 + step % kStages * kStageBytes;
-        const int64_t at = (int64_t)(four * kGroup + step % kGroup) * kStep;
+        uint8_t *to = stages + wave * 1024 + step % 2 * kStageBytes;
+        if ((stage + 1) * kStep > bytes) {        // half a stage, in the place of the other the same again
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+                from[i] -= chunk & 4 ? 64 : 0;
+        }
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int place = i < kLoadsA ? i * kT * 16 : TM * kStep + (i - kLoadsA) * kT * 16;
-            __builtin_amdgcn_global_load_lds((global_void *)(from[i] + at), (lds_void *)(to + place),
-                                             16, 0, 0);
+            (i < kLoadsA ? a : b).to_lds(to + place, from[i], stage * kStep);
         }
     };
     float16_tile acc[kMB][kNB] = {};
-#pragma unroll
-    for (int s = 0; s < kStages - 1; ++s)
-        if (s < steps)
-            fetch(s);
-    // A fragment: lane l holds 16 bytes of row l % 32, of a stage's four chunks number 2 (l / 32) first,
-    // then the one after it: the sum over k may take them in any order, and so the scales of a lane are
-    // two neighbours of the stage's four.
+    if (0 < steps)
+        fetch(0);
+    if (1 < steps)
+        fetch(1);
+    // A fragment: lane l holds 16 bytes of row l % 32. The sum over k may take a stage's eight chunks in
+    // any order: a lane takes numbers 4 (l / 32) to 4 (l / 32) + 3, whose scales are one word.
     const int frow = lane & 31, upper = lane >> 5;
     const uint8_t *const sa = stages + (wm * (TM / WM) + frow) * kStep;
     const uint8_t *const sb = stages + (TM + wn * (TN / WN) + frow) * kStep;
-    const uint8_t *const ca = scale_places + (wm * (TM / WM) + frow) * 16;
-    const uint8_t *const cb = scale_places + (TM + wn * (TN / WN) + frow) * 16;
-    const int at[2] = {swizzled(frow & 15, upper * 2) * 16, swizzled(frow & 15, upper * 2 + 1) * 16};
-    int4_t fa[2][kMB], fb[2][kNB];                // of both halves of a stage
+    const uint8_t *const ca = scale_places + (wm * (TM / WM) + frow) * 16 + upper * 4;
+    const uint8_t *const cb = scale_places + (TM + wn * (TN / WN) + frow) * 16 + upper * 4;
+    int4_t fa[2][kMB], fb[2][kNB];                // of a quarter of a stage and the next
     int ea[kMB], eb[kNB], next_a[kMB], next_b[kNB];       // scales of a stage and of the next
-    auto read = [&](int h, int step) {
-        const int stage = step % kStages * kStageBytes;
+    auto read = [&](auto quarter, int step) {
+        constexpr int h = decltype(quarter)::value;
+        const int at = step % 2 * kStageBytes + swizzled(frow & 15, upper * 4 + h) * 16;
 #pragma unroll
         for (int j = 0; j < kNB; ++j)
-            fb[h][j] = *(const int4_t *)(sb + stage + j * 32 * kStep + at[h]);
+            fb[h % 2][j] = *(const int4_t *)(sb + at + j * 32 * kStep);
 #pragma unroll
         for (int i = 0; i < kMB; ++i)
-            fa[h][i] = *(const int4_t *)(sa + stage + i * 32 * kStep + at[h]);
+            fa[h % 2][i] = *(const int4_t *)(sa + at + i * 32 * kStep);
     };
     auto read_scales = [&](int step) {
-        const int place = step / kGroup % 2 * kScaleBytes + step % kGroup * 4 + upper * 2;
+        const int stage = step * SPLIT + split;
+        const int place = (SPLIT > 1 ? step : step / 2) % 2 * kScaleBytes + stage % 2 * 8;
 #pragma unroll
         for (int j = 0; j < kNB; ++j)
-            next_b[j] = *(const uint16_t *)(cb + place + j * 32 * 16);
+            next_b[j] = *(const int *)(cb + place + j * 32 * 16);
 #pragma unroll
         for (int i = 0; i < kMB; ++i)
-            next_a[i] = *(const uint16_t *)(ca + place + i * 32 * 16);
+            next_a[i] = *(const int *)(ca + place + i * 32 * 16);
     };
-    auto multiply = [&](auto half) {
-        constexpr int h = decltype(half)::value;
+    // Of half a stage, the upper lanes' values have no part: with scales of 2^-127 on both sides their
+    // products, below 2^-243 in all, do not reach 32 bits.
+    auto take_scales = [&](int step) {
+        const bool in_k = (step * SPLIT + split) * kStep + upper * 64 < bytes;
+#pragma unroll
+        for (int j = 0; j < kNB; ++j)
+            eb[j] = in_k ? next_b[j] : 0;
+#pragma unroll
+        for (int i = 0; i < kMB; ++i)
+            ea[i] = in_k ? next_a[i] : 0;
+    };
+    auto multiply = [&](auto quarter) {
+        constexpr int h = decltype(quarter)::value;
 #pragma unroll
         for (int i = 0; i < kMB; ++i)
 #pragma unroll
             for (int j = 0; j < kNB; ++j)
-                acc[i][j] = multiply32<h>(fb[h][j], fa[h][i], acc[i][j], eb[j], ea[i]);
+                acc[i][j] = multiply32<h>(fb[h % 2][j], fa[h % 2][i], acc[i][j], eb[j], ea[i]);
         // One read after each of the first matrix instructions, so that none of them waits for it.
 #pragma unroll
-        for (int i = 0; i < 2 * (kMB + kNB) && i < kMB * kNB; ++i) {
+        for (int i = 0; i < (h == 3 ? 2 : 1) * (kMB + kNB) && i < kMB * kNB; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
     };
-    auto take_scales = [&] {
-#pragma unroll
-        for (int j = 0; j < kNB; ++j)
-            eb[j] = next_b[j];
-#pragma unroll
-        for (int i = 0; i < kMB; ++i)
-            ea[i] = next_a[i];
-    };
-    // Loads of the scales come on top of what is waited for at least: then a wait is for more than it
-    // needs.
-    if (steps >= kStages - 1)
-        __builtin_amdgcn_s_waitcnt(wait_loads((kStages - 2) * kLoads));
+    using std::integral_constant;
+    if (steps > 1)                                // the first stage and its scales are here
+        __builtin_amdgcn_s_waitcnt(wait_loads(kLoads));
     else
         __builtin_amdgcn_s_waitcnt(wait_loads(0));
     stage_barrier();
-    // The fragments that one half's matrix instructions take are read while the other half's run; so
-    // a step begins with its first half in registers and reads into the next stage at its end.
-    read(0, 0);
+    // The fragments that a quarter's matrix instructions take are read while the quarter before it is
+    // multiplied; so a step begins with its first quarter in registers and reads into the next stage
+    // at its end.
+    read(integral_constant<int, 0>(), 0);
     read_scales(0);
-    take_scales();
-    const int most = SPLIT == 1 ? steps         // of any group
-                                : (fours + SPLIT - 1) / SPLIT * kGroup + (fours % SPLIT ? 0 : rest);
+    take_scales(0);
     for (int step = 0; step < most; ++step) {
-        if (step + kStages - 2 < steps)
-            __builtin_amdgcn_s_waitcnt(wait_loads((kStages - 3) * kLoads));
-        else
-            __builtin_amdgcn_s_waitcnt(wait_loads(0));
-        // Every wavefront's loads of the next stage are in LDS, and the stage whose place is
-        // fetched into has been read by all.
+        const bool mine = SPLIT == 1 || step < steps;            // else others of the workgroup go on
+        if (mine) {
+            __builtin_amdgcn_sched_barrier(0);
+            read(integral_constant<int, 1>(), step);
+            multiply(integral_constant<int, 0>());
+            read(integral_constant<int, 2>(), step);
+            multiply(integral_constant<int, 1>());
+            read(integral_constant<int, 3>(), step);
+            multiply(integral_constant<int, 2>());
+        }
+        // The next stage is in LDS, and this one has been read by all.
+        __builtin_amdgcn_s_waitcnt(wait_loads(0));
         stage_barrier();
-        if (SPLIT > 1 && step >= steps)           // others of the workgroup go on
-            continue;
-        __builtin_amdgcn_sched_barrier(0);
-        read(1, step);
-        multiply(std::integral_constant<int, 0>());
-        if (step + kStages - 1 < steps)
-            fetch(step + kStages - 1);
-        __builtin_amdgcn_sched_barrier(0);
-        read(0, step + 1);                        // past the last step: not used
-        read_scales(step + 1);
-        multiply(std::integral_constant<int, 1>());
-        take_scales();
+        if (mine) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (step + 2 < steps)
+                fetch(step + 2);
+            __builtin_amdgcn_sched_barrier(0);
+            read(integral_constant<int, 0>(), step + 1);         // past the last step: not used
+            read_scales(step + 1);
+            multiply(integral_constant<int, 3>());
+            take_scales(step + 1);
+        }
     }
     stage_barrier();                              // the stages' LDS now holds results
     if constexpr (SPLIT > 1) {
@@ -571,12 +590,12 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void skinny_kernel(MxProductArgs
     }
 }
 
-template <typename TO, int TM, int TN, int WM, int WN, int SPLIT, int STAGES = 4>
+template <typename TO, int TM, int TN, int WM, int WN, int SPLIT>
 hipError_t launch_tiles(const MxProductArgs &p, hipStream_t stream) {
     const int64_t tm = (p.m + TM - 1) / TM, tn = (p.n + TN - 1) / TN;
     if (tm * tn * (64 * WM * WN * SPLIT) > (int64_t)UINT32_MAX)
         return hipErrorInvalidConfiguration;
-    tile_kernel<TO, TM, TN, WM, WN, SPLIT, STAGES>
+    tile_kernel<TO, TM, TN, WM, WN, SPLIT>
         <<<(unsigned)(tm * tn), 64 * WM * WN * SPLIT, 0, stream>>>(p, (uint32_t)tm, (uint32_t)tn);
     return hipGetLastError();
 }
@@ -592,6 +611,10 @@ hipError_t launch_skinny(const MxProductArgs &p, hipStream_t stream) {
 
 template <typename TO>
 hipError_t launch_product_type(const MxProductArgs &p, hipStream_t stream) {
+    for (int64_t stride : {p.m > 1 ? p.a_stride : 0, p.n > 1 ? p.b_stride : 0,
+                           p.m > 1 ? p.a_scales_stride : 0, p.n > 1 ? p.b_scales_stride : 0})
+        if (stride > kMaxStride)
+            return launch_skinny<TO>(p, stream);
     switch (mx_product_choice(p.m, p.n, p.k)) {
     case kMxSkinny: return launch_skinny<TO>(p, stream);
     case kMxTile64: return launch_tiles<TO, 64, 64, 2, 2, 4>(p, stream);

@@ -1,5 +1,8 @@
 // Which kernel computes a product of 4-bit rows: a rule on its sizes alone. Host code without HIP, so that
 // tests can ask it which kernel a call takes.
+//
+// Times below are in us for m x n x k, bf16 output, weights of two calls in turn; a / b: the kernel in
+// question against the next one.
 #pragma once
 
 #include <stdint.h>
@@ -8,36 +11,56 @@ namespace ccj {
 
 // Few results: 16 x 16 tiles, fragments straight from memory, k shared out over 8 wavefronts.
 constexpr int32_t kMxSkinny = 0;
-// Tiles through LDS, (rows x columns, groups that share out k).
-constexpr int32_t kMxTile64 = 1;         // 64 x 64, 4
-constexpr int32_t kMxTile128x64 = 2;     // 128 x 64, 2
-constexpr int32_t kMxTile128Split = 3;   // 128 x 128, 2
-constexpr int32_t kMxTile128 = 4;        // 128 x 128, 1
-constexpr int32_t kMxTile256 = 5;        // 256 x 256, 1
+// Tiles through LDS.
+constexpr int32_t kMxTile64 = 1;         // 64 x 64, two groups that share out k
+constexpr int32_t kMxTile128 = 2;        // 128 x 128
+constexpr int32_t kMxTile256 = 3;        // 256 x 256
 
 constexpr int64_t kMxUnits = 256;        // compute units
+
+// 32 x 4,096 x 4,096 6.6 / 6.9, 1 x 8,192 x 16,384 14.6 / 23.2, 16 x 8,192 x 8,192 12.4 / 13.3; of more
+// tiles 33 x 4,096 x 4,096 7.9 / 6.9, 1 x 32,000 x 4,096 13.2 / 12.4.
+constexpr int64_t kMxSkinnyTiles = 512;
+
+// A unit has two 64 x 64 tiles at a time: 512 x 4,096 x 16,384 38.8 / 45.8, 1,025 x 1,024 x 8,192 18.9 /
+// 24.2. A second round is too many: 512 x 8,192 x 4,096 23.3 / 16.0, 2,049 x 1,024 x 8,192 30.5 / 24.7.
+constexpr int64_t kMxTiles64 = 2 * kMxUnits;
+
+// A linear layer's rows that the skinny kernel puts in 4 bits itself, every tile again: the values that a
+// unit's tiles take together. 1 x 4,096 x 4,096 4.4 / 6.8 (the next being a launch for them), 8 x 4,096 x
+// 4,096 6.3 / 7.4, 1 x 16,384 x 4,096 10.1 / 11.9, 1 x 4,096 x 32,768 20.8 / 24.1; of more values 16 x 4,096
+// x 4,096 8.7 / 7.8, 4 x 8,192 x 8,192 15.2 / 13.9, of more tiles 1 x 32,000 x 2,048 11.9 / 10.6.
+constexpr int64_t kMxInsideRows = 16, kMxInsideTiles = 1024, kMxInsideValues = 32768;
+
+// Short products of 256 x 256 tiles have their loads and stores on their own.
+constexpr int64_t kMxLongK = 4096;
 
 inline int64_t mx_tiles(int64_t m, int64_t n, int64_t tm, int64_t tn) {
     return ((m + tm - 1) / tm) * ((n + tn - 1) / tn);
 }
 
 inline int32_t mx_product_choice(int64_t m, int64_t n, int64_t k) {
-    const int64_t t16 = mx_tiles(m, n, 16, 16);
-    if (t16 <= 256 || (t16 <= 512 && k <= 4096))
+    if (mx_tiles(m, n, 16, 16) <= kMxSkinnyTiles)
         return kMxSkinny;
-    // Larger tiles as soon as smaller ones would give a unit a second one.
-    if (mx_tiles(m, n, 64, 64) <= kMxUnits)
+    if (mx_tiles(m, n, 64, 64) <= kMxTiles64)
         return kMxTile64;
-    if (mx_tiles(m, n, 128, 64) <= kMxUnits)
-        return kMxTile128x64;
+    // A unit has two 128 x 128 tiles at a time or one of 256 x 256, which take 1.7 to 1.9 times as long:
+    // 4,096 x 4,096 x 1,024 22.2 in 128 x 128, 15.7 in 256 x 256; 4,300 x 4,100 x 8,192 100 / 120 (3 rounds
+    // against 2); of 13 rounds against 7 50,000 x 2,048 x 2,048 137 / 145, but x 8,192 575 / 484; 16,384 x
+    // 8,192 x 8,192 634 / 533.
     const int64_t t128 = mx_tiles(m, n, 128, 128), t256 = mx_tiles(m, n, 256, 256);
-    if (t128 <= kMxUnits)
-        return k >= 2048 ? kMxTile128Split : kMxTile128;
-    if (k <= 1024)
-        return kMxTile128;
-    // A unit has two 128 x 128 tiles at a time or one of 256 x 256.
     const int64_t r128 = (t128 + 2 * kMxUnits - 1) / (2 * kMxUnits), r256 = (t256 + kMxUnits - 1) / kMxUnits;
-    return 3 * r256 <= 2 * r128 ? kMxTile256 : kMxTile128;
+    return (k < kMxLongK ? 2 * r256 <= r128 : 5 * r256 <= 3 * r128) ? kMxTile256 : kMxTile128;
+}
+
+// Bytes of LDS that rows in 4 bits take there, with their scales.
+inline int64_t mx_quantize_lds(int64_t m, int64_t k) { return m * (k / 2 + 16 + k / 32 + 4); }
+
+// Whether a linear layer's rows are put in 4 bits by the skinny kernel; k a multiple of 128.
+inline bool mx_quantize_inside(int64_t m, int64_t n, int64_t k) {
+    const int64_t tiles = mx_tiles(m, n, 16, 16);
+    return m <= kMxInsideRows && tiles <= kMxInsideTiles &&
+           m * k * (tiles < kMxUnits ? kMxUnits : tiles) <= kMxInsideValues * kMxUnits;
 }
 
 }  // namespace ccj

@@ -69,6 +69,12 @@ __device__ __forceinline__ uint32_t max_with(uint32_t x) {
     return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, CONTROL, 0xf, 0xf, true));
 }
 
+// Block at `col` of a row, zeros behind its end.
+template <typename T>
+__device__ __forceinline__ Raw<T> row_block(const T *p, int col, int cols) {
+    return col + kCols <= cols ? load_block(p + col) : load_block(p + col, cols - col);
+}
+
 // The largest of four lanes that hold a block of 32 values.
 __device__ __forceinline__ uint32_t block_top(uint32_t x) {
     return max_with<quad_perm(2, 3, 0, 1)>(max_with<quad_perm(1, 0, 3, 2)>(x));
@@ -247,11 +253,18 @@ struct Rows {
     uint32_t bytes;
     __device__ Rows(const uint8_t *matrix, int64_t stride, int64_t first, int rows, int width)
         : p(matrix + first * stride), bytes((uint32_t)((rows - 1) * stride + width)) {}
-    // 16 bytes a lane to LDS, in the order of the lanes.
+    // 16 bytes a lane to LDS, in the order of the lanes. In assembly, as the compiler would wait for
+    // all such loads before any read of LDS, and with them for the stage that was asked for last; the
+    // kernel's own waits are what orders them. The operand registers are ready after 5 wait states
+    // whatever wrote them, m0 after one.
     __device__ __forceinline__ void to_lds(uint8_t *lds, uint32_t at, int more) const {
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(
-            __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p), 0, (int)bytes, 0x20000),
-            (lds_void *)lds, 16, at, more, 0, 0);
+        const uint64_t address = (uint64_t)(uintptr_t)p;
+        const int4_t buffer = {(int)(uint32_t)address, (int)(uint32_t)(address >> 32) & 0xffff,
+                               (int)bytes, 0x20000};
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                     :
+                     : "s"((uint32_t)(uintptr_t)(lds_void *)lds), "v"(at), "s"(buffer), "s"(more)
+                     : "memory", "m0");
     }
 };
 
@@ -378,17 +391,17 @@ __global__ __launch_bounds__(64 * WM * WN * SPLIT, TM * TN / (WM * WN) > 8192 ? 
     const uint8_t *const sb = stages + (TM + wn * (TN / WN) + frow) * kStep;
     const uint8_t *const ca = scale_places + (wm * (TM / WM) + frow) * 16 + upper * 4;
     const uint8_t *const cb = scale_places + (TM + wn * (TN / WN) + frow) * 16 + upper * 4;
-    int4_t fa[2][kMB], fb[2][kNB];                // of a quarter of a stage and the next
+    int4_t fa[4][kMB], fb[4][kNB];                // of a stage's quarters
     int ea[kMB], eb[kNB], next_a[kMB], next_b[kNB];       // scales of a stage and of the next
     auto read = [&](auto quarter, int step) {
         constexpr int h = decltype(quarter)::value;
         const int at = step % 2 * kStageBytes + swizzled(frow & 15, upper * 4 + h) * 16;
 #pragma unroll
         for (int j = 0; j < kNB; ++j)
-            fb[h % 2][j] = *(const int4_t *)(sb + at + j * 32 * kStep);
+            fb[h][j] = *(const int4_t *)(sb + at + j * 32 * kStep);
 #pragma unroll
         for (int i = 0; i < kMB; ++i)
-            fa[h % 2][i] = *(const int4_t *)(sa + at + i * 32 * kStep);
+            fa[h][i] = *(const int4_t *)(sa + at + i * 32 * kStep);
     };
     auto read_scales = [&](int step) {
         const int stage = step * SPLIT + split;
@@ -417,14 +430,24 @@ __global__ __launch_bounds__(64 * WM * WN * SPLIT, TM * TN / (WM * WN) > 8192 ? 
         for (int i = 0; i < kMB; ++i)
 #pragma unroll
             for (int j = 0; j < kNB; ++j)
-                acc[i][j] = multiply32<h>(fb[h % 2][j], fa[h % 2][i], acc[i][j], eb[j], ea[i]);
-        // One read after each of the first matrix instructions, so that none of them waits for it.
+                acc[i][j] = multiply32<h>(fb[h][j], fa[h][i], acc[i][j], eb[j], ea[i]);
+        // The reads of LDS between the first quarter's and the last one's matrix instructions.
+        if (h == 0 || h == 3)
 #pragma unroll
-        for (int i = 0; i < (h == 3 ? 2 : 1) * (kMB + kNB) && i < kMB * kNB; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        }
+            for (int i = 0; i < kMB * kNB; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, h == 0 ? 3 : 2, 0);
+            }
         __builtin_amdgcn_sched_barrier(0);
+    };
+    // The matrix instructions above stay above: nothing in the program keeps them from moving down past
+    // the barrier to the next use of their results, behind the reads that they are to overlap.
+    auto pin = [&] {
+#pragma unroll
+        for (int i = 0; i < kMB; ++i)
+#pragma unroll
+            for (int j = 0; j < kNB; ++j)
+                asm volatile("" : "+v"(acc[i][j]));
     };
     using std::integral_constant;
     if (steps > 1)                                // the first stage and its scales are here
@@ -432,9 +455,9 @@ __global__ __launch_bounds__(64 * WM * WN * SPLIT, TM * TN / (WM * WN) > 8192 ? 
     else
         __builtin_amdgcn_s_waitcnt(wait_loads(0));
     stage_barrier();
-    // The fragments that a quarter's matrix instructions take are read while the quarter before it is
-    // multiplied; so a step begins with its first quarter in registers and reads into the next stage
-    // at its end.
+    // A step begins with its first quarter in registers. While that is multiplied the others are read,
+    // so that the stage's place is free, and the stage after the next on its way, before three quarters
+    // of the matrix instructions; the next stage, which was asked for a step ago, is here by then.
     read(integral_constant<int, 0>(), 0);
     read_scales(0);
     take_scales(0);
@@ -443,20 +466,19 @@ __global__ __launch_bounds__(64 * WM * WN * SPLIT, TM * TN / (WM * WN) > 8192 ? 
         if (mine) {
             __builtin_amdgcn_sched_barrier(0);
             read(integral_constant<int, 1>(), step);
-            multiply(integral_constant<int, 0>());
             read(integral_constant<int, 2>(), step);
-            multiply(integral_constant<int, 1>());
             read(integral_constant<int, 3>(), step);
-            multiply(integral_constant<int, 2>());
+            multiply(integral_constant<int, 0>());
+            pin();
         }
-        // The next stage is in LDS, and this one has been read by all.
         __builtin_amdgcn_s_waitcnt(wait_loads(0));
         stage_barrier();
         if (mine) {
-            __builtin_amdgcn_sched_barrier(0);
             if (step + 2 < steps)
                 fetch(step + 2);
             __builtin_amdgcn_sched_barrier(0);
+            multiply(integral_constant<int, 1>());
+            multiply(integral_constant<int, 2>());
             read(integral_constant<int, 0>(), step + 1);         // past the last step: not used
             read_scales(step + 1);
             multiply(integral_constant<int, 3>());
@@ -540,35 +562,73 @@ constexpr int kSkinnyWaves = 8;
 // come from memory to registers as the matrix instruction takes them. A lane's four blocks of a slab
 // follow each other, 64 bytes and one word of scales; the sum over k may take its blocks in any order.
 // The wavefronts' sums meet in LDS.
-template <typename TO>
-__global__ __launch_bounds__(64 * kSkinnyWaves) void skinny_kernel(MxProductArgs p) {
-    constexpr int kSlab = 256;                    // bytes
+//
+// QUANT: the rows of a (at most 16) are put in 4 bits from x in the kernel, by every workgroup again: a
+// few KiB from L2 on the weights' way, against a launch of their own.
+template <typename TO, bool QUANT>
+__global__ __launch_bounds__(64 * kSkinnyWaves) void skinny_kernel(MxProductArgs p, MxRowsArgs x,
+                                                                   Divider div) {
+    constexpr int kSlab = 256, kT = 64 * kSkinnyWaves;           // bytes; threads
+    extern __shared__ __attribute__((aligned(16))) uint8_t quantized[];
     __shared__ __attribute__((aligned(16))) float part[kSkinnyWaves][256];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t tiles_n = (uint32_t)((p.n + 15) / 16);
     const int64_t m0 = (int64_t)(blockIdx.x / tiles_n) * 16, n0 = (int64_t)(blockIdx.x % tiles_n) * 16;
     const int bytes = (int)(p.k / 2), piece = (lane >> 4) * 64;
     const int64_t row_a = min(m0 + (lane & 15), p.m - 1), row_b = min(n0 + (lane & 15), p.n - 1);
-    const uint8_t *a = p.a + row_a * p.a_stride, *b = p.b + row_b * p.b_stride;
-    const uint8_t *sa = p.a_scales + row_a * p.a_scales_stride;
+    // Rows in LDS are 16 bytes longer, against bank conflicts; their scales lie behind them.
+    const int pitch = bytes + 16, scale_pitch = bytes / 16 + 4;
+    uint8_t *const quantized_scales = quantized + (QUANT ? p.m * pitch : 0);
+    const uint8_t *a = QUANT ? quantized + row_a * pitch : p.a + row_a * p.a_stride;
+    const uint8_t *sa = QUANT ? quantized_scales + row_a * scale_pitch
+                              : p.a_scales + row_a * p.a_scales_stride;
+    const uint8_t *b = p.b + row_b * p.b_stride;
     const uint8_t *sb = p.b_scales + row_b * p.b_scales_stride;
-    float4_t acc = {};
-    for (int k0 = wave * kSlab; k0 < bytes; k0 += kSkinnyWaves * kSlab) {
-        // Pieces past k repeat the row's first one; of a they count as zeros, and their scales as 0.
-        const int at = k0 + piece;
-        const bool in = at < bytes;
-        int4_t fa[4], fb[4];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            fb[c] = *(const int4_t *)(b + (in ? at : 0) + c * 16);
-            fa[c] = *(const int4_t *)(a + (in ? at : 0) + c * 16);
-        }
-        int scale_a = *(const int *)(sa + (in ? at / 16 : 0)), scale_b = *(const int *)(sb + (in ? at / 16 : 0));
-        scale_a = in ? scale_a : 0;
-        scale_b = in ? scale_b : 0;
+    // Pieces past k repeat the row's first one, with scales of 2^-127 on both sides: their products,
+    // below 2^-243 in all, do not reach 32 bits.
+    auto read = [&](const uint8_t *from, const uint8_t *scales, int4_t (&f)[4], int &scale, int k0) {
+        const int at = k0 + piece < bytes ? k0 + piece : 0;
 #pragma unroll
         for (int c = 0; c < 4; ++c)
-            fa[c] = in ? fa[c] : int4_t{};
+            f[c] = *(const int4_t *)(from + at + c * 16);
+        scale = *(const int *)(scales + at / 16);
+        scale = k0 + piece < bytes ? scale : 0;
+    };
+    int4_t fa[4], fb[4];
+    int scale_a, scale_b;
+    const int first = wave * kSlab;
+    if (first < bytes)
+        read(b, sb, fb, scale_b, first);
+    if constexpr (QUANT) {
+        constexpr int kU = 4;                     // blocks of 8 columns of a thread on their way
+        const int blocks = bytes / 4, units = (int)p.m * blocks;
+        for (int unit0 = threadIdx.x; unit0 < units; unit0 += kT * kU) {
+            Raw<TO> v[kU];
+#pragma unroll
+            for (int u = 0; u < kU; ++u) {
+                const int unit = min(unit0 + u * kT, units - 4 + (int)(threadIdx.x & 3));
+                const int row = div(unit), col = (unit - row * blocks) * kCols;
+                v[u] = row_block((const TO *)((const char *)x.x + row * x.x_stride), col, x.cols);
+            }
+#pragma unroll
+            for (int u = 0; u < kU; ++u) {
+                const uint32_t byte = scale_byte(block_top(top_of(v[u])));
+                const int unit = unit0 + u * kT;
+                if (unit < units) {
+                    const int row = div(unit), block = unit - row * blocks;
+                    *(uint32_t *)(quantized + row * pitch + block * 4) = four_bits(v[u], byte);
+                    if (block % 4 == 0)
+                        quantized_scales[row * scale_pitch + block / 4] = (uint8_t)byte;
+                }
+            }
+        }
+        __syncthreads();
+    }
+    float4_t acc = {};
+    for (int k0 = first; k0 < bytes; k0 += kSkinnyWaves * kSlab) {
+        if (k0 != first)
+            read(b, sb, fb, scale_b, k0);
+        read(a, sa, fa, scale_a, k0);
         acc = multiply16<0>(fb[0], fa[0], acc, scale_b, scale_a);
         acc = multiply16<1>(fb[1], fa[1], acc, scale_b, scale_a);
         acc = multiply16<2>(fb[2], fa[2], acc, scale_b, scale_a);
@@ -602,10 +662,11 @@ hipError_t launch_tiles(const MxProductArgs &p, hipStream_t stream) {
 
 template <typename TO>
 hipError_t launch_skinny(const MxProductArgs &p, hipStream_t stream) {
-    const int64_t tiles = (p.m + 15) / 16 * ((p.n + 15) / 16);
+    const int64_t tiles = mx_tiles(p.m, p.n, 16, 16);
     if (tiles * (64 * kSkinnyWaves) > (int64_t)UINT32_MAX)
         return hipErrorInvalidConfiguration;
-    skinny_kernel<TO><<<(unsigned)tiles, 64 * kSkinnyWaves, 0, stream>>>(p);
+    skinny_kernel<TO, false><<<(unsigned)tiles, 64 * kSkinnyWaves, 0, stream>>>(p, MxRowsArgs{},
+                                                                                Divider(1));
     return hipGetLastError();
 }
 
@@ -617,12 +678,22 @@ hipError_t launch_product_type(const MxProductArgs &p, hipStream_t stream) {
             return launch_skinny<TO>(p, stream);
     switch (mx_product_choice(p.m, p.n, p.k)) {
     case kMxSkinny: return launch_skinny<TO>(p, stream);
-    case kMxTile64: return launch_tiles<TO, 64, 64, 2, 2, 4>(p, stream);
-    case kMxTile128x64: return launch_tiles<TO, 128, 64, 2, 2, 2>(p, stream);
-    case kMxTile128Split: return launch_tiles<TO, 128, 128, 2, 2, 2>(p, stream);
+    case kMxTile64: return launch_tiles<TO, 64, 64, 2, 2, 2>(p, stream);
     case kMxTile128: return launch_tiles<TO, 128, 128, 2, 2, 1>(p, stream);
     default: return launch_tiles<TO, 256, 256, 2, 4, 1>(p, stream);
     }
+}
+
+template <typename T>
+hipError_t launch_linear_type(const MxRowsArgs &x, const MxProductArgs &p, hipStream_t stream) {
+    if (mx_quantize_inside(p.m, p.n, p.k)) {
+        const int64_t tiles = mx_tiles(p.m, p.n, 16, 16);
+        skinny_kernel<T, true><<<(unsigned)tiles, 64 * kSkinnyWaves, mx_quantize_lds(p.m, p.k),
+                                 stream>>>(p, x, Divider((uint32_t)(p.k / kCols)));
+        return hipGetLastError();
+    }
+    const hipError_t e = quantize_type<T>(x, stream);
+    return e == hipSuccess ? launch_product_type<T>(p, stream) : e;
 }
 
 }  // namespace
@@ -652,8 +723,11 @@ hipError_t launch_mx_product(const MxProductArgs &p, hipStream_t stream) {
 }
 
 hipError_t launch_mx_linear(const MxRowsArgs &x, const MxProductArgs &p, hipStream_t stream) {
-    const hipError_t e = launch_mx_quantize(x, stream);
-    return e == hipSuccess ? launch_mx_product(p, stream) : e;
+    switch (x.type) {
+    case kF32: return launch_linear_type<float>(x, p, stream);
+    case kF16: return launch_linear_type<half_t>(x, p, stream);
+    default: return launch_linear_type<bf16_t>(x, p, stream);
+    }
 }
 
 }  // namespace ccj

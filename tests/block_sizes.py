@@ -1,0 +1,19 @@
+"""Sizes that reach every kernel of the 4-bit products and of the block norms: the GPU tests run them, the CPU
+tests of the choices (csrc/mx_choice.h, csrc/norm_choice.h) check that nothing is left out."""
+
+# m, n, k of a 4-bit product and the kernel that mx_choice.h takes for it: partial tiles in both directions,
+# k of less than a stage, of one, of half a stage more, of two stages and more than are on the way.
+SKINNY, TILE64, TILE128, TILE256 = range(4)
+PRODUCTS = [
+    (5, 3_001, 640, SKINNY), (40, 1_000, 8_320, SKINNY), (17, 4_096, 5_000, SKINNY),
+    (1_000, 1_001, 128, TILE64), (333, 1_030, 2_055, TILE64), (1_020, 2_047, 256, TILE64),
+    (700, 900, 384, TILE64), (600, 777, 512, TILE64), (65, 4_100, 1_664, TILE64), (800, 1_000, 9_000, TILE64),
+    (4_100, 1_030, 96, TILE128), (2_050, 1_200, 256, TILE128), (2_100, 1_281, 384, TILE128),
+    (300, 9_001, 640, TILE128), (50_000, 65, 300, TILE128), (2_300, 3_300, 2_176, TILE128),
+    (3_000, 3_001, 128, TILE256), (2_999, 3_100, 256, TILE256), (4_003, 2_500, 384, TILE256),
+    (2_049, 4_290, 1_152, TILE256), (10_000, 1_000, 4_224, TILE256), (16_389, 5_001, 4_096, TILE256),
+]
+
+# Linear layers whose rows the skinny kernel puts in 4 bits itself, and some just past its limits.
+INSIDE = [(1, 500, 32_768), (16, 640, 2_048), (13, 555, 2_400), (1, 16_384, 4_096), (7, 300, 4_600), (2, 9_000, 99)]
+OUTSIDE = [(1, 500, 32_769), (16, 640, 2_049), (1, 16_400, 96), (17, 64, 96), (16, 4_097, 2_048)]

@@ -67,7 +67,7 @@ struct RowSum {
 
 // ---- blocks of 8 columns ----
 
-// Block at `col` of a vector of `cols` floats, `other` behind its end or without a vector.
+// Block at `col` of a vector of `cols` floats, `other` without a vector, 0 behind the end.
 __device__ __forceinline__ void vector_block(const float *v, int col, int cols, float other,
                                              float (&x)[kCols]) {
     if (v && col + kCols <= cols) {
@@ -78,8 +78,17 @@ __device__ __forceinline__ void vector_block(const float *v, int col, int cols, 
     } else {
 #pragma unroll
         for (int i = 0; i < kCols; ++i)
-            x[i] = v && col + i < cols ? v[col + i] : other;
+            x[i] = col + i >= cols ? 0.0f : v ? v[col + i] : other;
     }
+}
+
+// A block of a row that its lanes hold: where lanes exchange pieces of 32-bit elements, settle() puts
+// them in place. TAIL: rows have a last block of fewer columns, or are not aligned to 16 bytes.
+template <bool TAIL, typename T>
+__device__ __forceinline__ Raw<T> held_block(const T *row, int col, int cols, int exchange) {
+    if (col + kCols <= cols)
+        return load_pieces<!TAIL>(row + col, exchange);
+    return TAIL && col < cols ? load_block(row + col, cols - col) : Raw<T>{};
 }
 
 // Block at `col` of a row, zeros behind its end.
@@ -94,6 +103,15 @@ __device__ __forceinline__ void put_block(T *p, int col, int cols, const float (
         store_block(p + col, x);
     else
         store_block(p + col, x, cols - col);
+}
+
+template <bool TAIL, typename T>
+__device__ __forceinline__ void put_held(T *row, int col, int cols, int exchange,
+                                         const float (&x)[kCols]) {
+    if (!TAIL && col < cols)
+        stream_block(row + col, x, exchange);
+    else if (TAIL && col < cols)
+        put_block(row, col, cols, x);
 }
 
 // A row's norm: (v - mean) * r.

@@ -46,6 +46,152 @@ struct Gradient : Forward<T, S> {
     }
 };
 
+// ---- rows in registers ----
+
+// L lanes of a row hold a block of 8 columns each, and for all the rows that they go through the weights of
+// their columns and the sums over rows. One read of f, gate, x, dy and dh, one write of dx, df and dgate;
+// four sums over the row's lanes one after another, two more with layer norms. At the end the groups of
+// lanes of a workgroup add up their sums in order. BIAS: with post's bias or the sums of either bias.
+// partial: [workgroups][kSums][padded columns].
+template <typename T, typename S, int L, bool TAIL, bool BIAS>
+__global__ __launch_bounds__(L < kThreads ? kThreads : L) void row_grad_kernel(NormGradArgs ga,
+                                                                               float *partial,
+                                                                               int64_t padded) {
+    const NormArgs &a = ga.a;
+    constexpr int kT = L < kThreads ? kThreads : L, kGroups = kT / L;
+    constexpr int kV = BIAS ? kSums : 2;          // of Sum, the biases come last
+    __shared__ float place[2][L > 64 ? L / 64 : 1][2];
+    RowSum<L, 2> sum{place};
+    const int lane = threadIdx.x % L, col = lane * kCols, exchange = exchange_of(lane, a.cols);
+    const float cols = (float)a.cols;
+    float w[kCols], b[kCols] = {}, q[kCols], sums[kV][kCols] = {};
+    vector_block(a.post_weight, col, a.cols, 1.0f, w);
+    if (BIAS)
+        vector_block(a.post_bias, col, a.cols, 0.0f, b);
+    vector_block(a.pre_weight, col, a.cols, 1.0f, q);
+    auto in = [&](int e) { return col + (TAIL ? e : 0) < a.cols; };
+    for (int64_t row = (int64_t)blockIdx.x * kGroups + threadIdx.x / L; row < a.n;
+         row += (int64_t)gridDim.x * kGroups) {
+        auto held = [&](auto type, const void *p, int64_t stride) {
+            using E = decltype(type);
+            return p ? held_block<TAIL>(row_of<E>(p, stride, row), col, a.cols, exchange) : Raw<E>{};
+        };
+        Raw<T> f = held(T(), a.f, a.f_stride), u = held(T(), a.gate, a.gate_stride);
+        Raw<S> x = held(S(), a.x, a.x_stride);
+        Raw<T> dh = held(T(), ga.dh, ga.dh_stride);
+        Raw<S> dy = held(S(), ga.dy, ga.dy_stride);
+        settle(f, exchange);
+        RowStats st = {};
+        if (a.post == kNormLayer) {
+            float s = 0.0f;
+#pragma unroll
+            for (int e = 0; e < kCols; ++e)
+                s += (float)f[e];
+            st.post.mean = sum(s) / cols;
+        }
+        if (a.post != kNormNone) {
+            float s = 0.0f;
+#pragma unroll
+            for (int e = 0; e < kCols; ++e) {
+                const float d = (float)f[e] - st.post.mean;
+                s += in(e) ? d * d : 0.0f;
+            }
+            st.post.r = inverse_size(sum(s), a.cols, a.post_eps);
+        }
+        settle(u, exchange);
+        settle(x, exchange);
+        Gradient<T, S> p;
+        p(a, f, u, x, st.post, w, b);
+        if (a.pre == kNormLayer) {
+            float s = 0.0f;
+#pragma unroll
+            for (int e = 0; e < kCols; ++e)
+                s += p.y[e];                      // 0 where the row has no column
+            st.pre.mean = sum(s) / cols;
+        }
+        if (a.pre != kNormNone) {
+            float s = 0.0f;
+#pragma unroll
+            for (int e = 0; e < kCols; ++e) {
+                const float d = p.y[e] - st.pre.mean;
+                s += in(e) ? d * d : 0.0f;
+            }
+            st.pre.r = inverse_size(sum(s), a.cols, a.pre_eps);
+        }
+        settle(dh, exchange);
+        settle(dy, exchange);
+        p.of_pre(dh, q, st.pre);
+        if (a.pre != kNormNone) {
+            float s[2] = {};
+#pragma unroll
+            for (int e = 0; e < kCols; ++e) {
+                s[0] += p.t[e];
+                s[1] += p.t[e] * p.yn[e];
+            }
+            sum(s);
+            st.t = a.pre == kNormLayer ? s[0] / cols : 0.0f;
+            st.t_yn = s[1] / cols;
+        }
+        p.of_sum(ga, dy, st);
+        p.of_post(ga, w);
+        if (a.post != kNormNone) {
+            float s[2] = {};
+#pragma unroll
+            for (int e = 0; e < kCols; ++e) {
+                s[0] += p.v[e];
+                s[1] += p.v[e] * p.fn[e];
+            }
+            sum(s);
+            st.v = a.post == kNormLayer ? s[0] / cols : 0.0f;
+            st.v_fn = s[1] / cols;
+        }
+        float df[kCols], du[kCols];
+#pragma unroll
+        for (int e = 0; e < kCols; ++e) {
+            const float d = p.dy[e] * a.scale;
+            df[e] = a.post == kNormNone ? p.v[e] : st.post.r * (p.v[e] - st.v - p.fn[e] * st.v_fn);
+            du[e] = d * p.n[e] * p.slope[e];
+            sums[kPostWeight][e] += d * p.g[e] * p.fn[e];
+            sums[kPreWeight][e] += (float)dh[e] * p.yn[e];
+            if (BIAS) {
+                sums[kPostBias][e] += d * p.g[e];
+                sums[kPreBias][e] += (float)dh[e];
+            }
+        }
+        if (ga.dx)
+            put_held<TAIL>(row_of<S>(ga.dx, ga.dx_stride, row), col, a.cols, exchange, p.dy);
+        if (ga.dgate)
+            put_held<TAIL>(row_of<T>(ga.dgate, ga.dgate_stride, row), col, a.cols, exchange, du);
+        put_held<TAIL>(row_of<T>(ga.df, ga.df_stride, row), col, a.cols, exchange, df);
+    }
+    if constexpr (kGroups == 1) {
+        if (col < a.cols)
+#pragma unroll
+            for (int v = 0; v < kV; ++v)
+                if (ga.sums[v])
+                    store_block(partial + ((int64_t)blockIdx.x * kSums + v) * padded + col, sums[v]);
+    } else {
+        __shared__ float part[kGroups][L * kCols];
+#pragma unroll
+        for (int v = 0; v < kV; ++v) {
+            if (!ga.sums[v])
+                continue;
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < kCols; ++e)
+                part[threadIdx.x / L][col + e] = sums[v][e];
+            __syncthreads();
+            for (int c = threadIdx.x; c < a.cols; c += kT) {
+                float s = 0.0f;
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g)
+                    s += part[g][c];
+                partial[((int64_t)blockIdx.x * kSums + v) * padded + c] = s;
+            }
+        }
+    }
+}
+
 // ---- rows of any length ----
 
 // Each row's statistics, a workgroup a row: passes over the row as in the forward kernel, then one for
@@ -255,8 +401,40 @@ hipError_t fold(const NormGradArgs &g, const float *partial, int64_t strips, hip
     return hipGetLastError();
 }
 
+template <typename T, typename S, int L>
+hipError_t launch_rows(const NormGradArgs &g, hipStream_t stream) {
+    const NormArgs &a = g.a;
+    constexpr int kT = L < kThreads ? kThreads : L;
+    const int64_t padded = padded_cols(a.cols), groups = norm_grad_groups(a.n, a.cols);
+    float *partial = static_cast<float *>(g.workspace);
+    auto even = [](const void *p, int64_t stride) { return !p || even_rows(p, stride); };
+    const bool tail = !(a.cols % kCols == 0 && even(a.f, a.f_stride) && even(a.x, a.x_stride) &&
+                        even(a.gate, a.gate_stride) && even(g.dy, g.dy_stride) &&
+                        even(g.dh, g.dh_stride) && even(g.dx, g.dx_stride) &&
+                        even(g.df, g.df_stride) && even(g.dgate, g.dgate_stride));
+    const bool bias = a.post_bias || g.sums[kPostBias] || g.sums[kPreBias];
+    const unsigned grid = (unsigned)groups;
+    if (tail && bias)
+        row_grad_kernel<T, S, L, true, true><<<grid, kT, 0, stream>>>(g, partial, padded);
+    else if (tail)
+        row_grad_kernel<T, S, L, true, false><<<grid, kT, 0, stream>>>(g, partial, padded);
+    else if (bias)
+        row_grad_kernel<T, S, L, false, true><<<grid, kT, 0, stream>>>(g, partial, padded);
+    else
+        row_grad_kernel<T, S, L, false, false><<<grid, kT, 0, stream>>>(g, partial, padded);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? fold(g, partial, groups, stream) : e;
+}
+
 template <typename T, typename S>
 hipError_t launch_types(const NormGradArgs &g, hipStream_t stream) {
+    switch (norm_grad_lanes(g.a.cols)) {
+    case 16: return launch_rows<T, S, 16>(g, stream);
+    case 64: return launch_rows<T, S, 64>(g, stream);
+    case 256: return launch_rows<T, S, 256>(g, stream);
+    case 512: return launch_rows<T, S, 512>(g, stream);
+    case 1024: return launch_rows<T, S, 1024>(g, stream);
+    }
     const int64_t padded = padded_cols(g.a.cols), strips = norm_wide_strips(g.a.n, g.a.cols);
     RowStats *stats = static_cast<RowStats *>(g.workspace);
     float *partial = reinterpret_cast<float *>(stats + g.a.n);
@@ -274,6 +452,8 @@ hipError_t launch_types(const NormGradArgs &g, hipStream_t stream) {
 }  // namespace
 
 int64_t norm_grad_workspace_bytes(int64_t n, int32_t cols) {
+    if (norm_grad_lanes(cols))
+        return norm_grad_groups(n, cols) * kSums * padded_cols(cols) * 4;
     return n * (int64_t)sizeof(RowStats) + norm_wide_strips(n, cols) * kSums * padded_cols(cols) * 4;
 }
 

@@ -1,10 +1,97 @@
 // Norms after and before a block, with its gate and residual sum: rows in, rows out.
+#include "norm_choice.h"
 #include "norm_device.h"
 
 namespace ccj {
 namespace {
 
 constexpr int kThreads = 256;
+
+// Rows that stay in registers: L lanes of a row hold B blocks of 8 columns each, and weights and biases of
+// their columns for all the rows that they go through. One read of f, gate and x, one write of y and h;
+// the sums between them are over lanes, and over a workgroup's wavefronts through LDS.
+template <typename T, typename S, int L, int B, bool TAIL>
+__global__ __launch_bounds__(L < kThreads ? kThreads : L) void row_norm_kernel(NormArgs a) {
+    constexpr int kT = L < kThreads ? kThreads : L, kGroups = kT / L;
+    __shared__ float place[2][L > 64 ? L / 64 : 1][1];
+    RowSum<L, 1> sum{place};
+    const int lane = threadIdx.x % L;
+    int col[B], exchange[B];
+    float post_w[B][kCols], post_b[B][kCols], pre_w[B][kCols], pre_b[B][kCols];
+#pragma unroll
+    for (int i = 0; i < B; ++i) {
+        col[i] = (lane + i * L) * kCols;
+        exchange[i] = exchange_of(lane + i * L, a.cols);
+        vector_block(a.post_weight, col[i], a.cols, 1.0f, post_w[i]);
+        vector_block(a.post_bias, col[i], a.cols, 0.0f, post_b[i]);
+        vector_block(a.pre_weight, col[i], a.cols, 1.0f, pre_w[i]);
+        vector_block(a.pre_bias, col[i], a.cols, 0.0f, pre_b[i]);
+    }
+    // The sum over a row of use(block, element) where it has a column.
+    auto over = [&](auto &&use) {
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < B; ++i)
+#pragma unroll
+            for (int e = 0; e < kCols; ++e)
+                s += col[i] + (TAIL ? e : 0) < a.cols ? use(i, e) : 0.0f;
+        return sum(s);
+    };
+    for (int64_t row = (int64_t)blockIdx.x * kGroups + threadIdx.x / L; row < a.n;
+         row += (int64_t)gridDim.x * kGroups) {
+        Raw<T> f[B], u[B];
+        Raw<S> x[B];
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+            f[i] = held_block<TAIL>(row_of<T>(a.f, a.f_stride, row), col[i], a.cols, exchange[i]);
+            u[i] = Raw<T>{};
+            x[i] = Raw<S>{};
+            if (a.gate)
+                u[i] = held_block<TAIL>(row_of<T>(a.gate, a.gate_stride, row), col[i], a.cols,
+                                        exchange[i]);
+            if (a.x)
+                x[i] = held_block<TAIL>(row_of<S>(a.x, a.x_stride, row), col[i], a.cols, exchange[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < B; ++i)
+            settle(f[i], exchange[i]);
+        RowNorm post, pre;
+        if (a.post == kNormLayer)
+            post.mean = over([&](int i, int e) { return (float)f[i][e]; }) / (float)a.cols;
+        if (a.post != kNormNone)
+            post.r = inverse_size(over([&](int i, int e) {
+                                      const float d = (float)f[i][e] - post.mean;
+                                      return d * d;
+                                  }),
+                                  a.cols, a.post_eps);
+        Forward<T, S> p[B];
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+            settle(u[i], exchange[i]);
+            settle(x[i], exchange[i]);
+            p[i](a, f[i], u[i], x[i], post, post_w[i], post_b[i]);
+            put_held<TAIL>(row_of<S>(a.y, a.y_stride, row), col[i], a.cols, exchange[i], p[i].y);
+        }
+        if (!a.h)
+            continue;
+        if (a.pre == kNormLayer)
+            pre.mean = over([&](int i, int e) { return p[i].y[e]; }) / (float)a.cols;
+        if (a.pre != kNormNone)
+            pre.r = inverse_size(over([&](int i, int e) {
+                                     const float d = p[i].y[e] - pre.mean;
+                                     return d * d;
+                                 }),
+                                 a.cols, a.pre_eps);
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+            float h[kCols];
+#pragma unroll
+            for (int e = 0; e < kCols; ++e)
+                h[e] = (p[i].y[e] - pre.mean) * pre.r * pre_w[i][e] + pre_b[i][e];
+            put_held<TAIL>(row_of<T>(a.h, a.h_stride, row), col[i], a.cols, exchange[i], h);
+        }
+    }
+}
 
 // Rows of any length, a workgroup each, in pieces of 2,048 columns: a pass over f for each sum of its
 // norm, a pass over x, f and the gate for each sum of y's, and one that writes. All but the first pass
@@ -89,8 +176,33 @@ __global__ __launch_bounds__(kThreads) void wide_norm_kernel(NormArgs a) {
     }
 }
 
+template <typename T, typename S, int L, int B>
+hipError_t launch_rows(const NormArgs &a, hipStream_t stream) {
+    constexpr int kT = L < kThreads ? kThreads : L, kGroups = kT / L;
+    const int64_t groups = (a.n + kGroups - 1) / kGroups, most = 256 * (2048 / kT);
+    const unsigned grid = (unsigned)(groups < most ? groups : most);
+    const bool even = a.cols % kCols == 0 && even_rows(a.f, a.f_stride) && even_rows(a.y, a.y_stride) &&
+                      (!a.x || even_rows(a.x, a.x_stride)) && (!a.h || even_rows(a.h, a.h_stride)) &&
+                      (!a.gate || even_rows(a.gate, a.gate_stride));
+    if (even)
+        row_norm_kernel<T, S, L, B, false><<<grid, kT, 0, stream>>>(a);
+    else
+        row_norm_kernel<T, S, L, B, true><<<grid, kT, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
 template <typename T, typename S>
 hipError_t launch_types(const NormArgs &a, hipStream_t stream) {
+    const NormShape shape = norm_shape(a.cols);
+    switch (shape.lanes * 4 + shape.blocks) {
+    case 16 * 4 + 1: return launch_rows<T, S, 16, 1>(a, stream);
+    case 64 * 4 + 1: return launch_rows<T, S, 64, 1>(a, stream);
+    case 64 * 4 + 2: return launch_rows<T, S, 64, 2>(a, stream);
+    case 256 * 4 + 1: return launch_rows<T, S, 256, 1>(a, stream);
+    case 256 * 4 + 2: return launch_rows<T, S, 256, 2>(a, stream);
+    case 512 * 4 + 2: return launch_rows<T, S, 512, 2>(a, stream);
+    case 1024 * 4 + 2: return launch_rows<T, S, 1024, 2>(a, stream);
+    }
     const int64_t most = 1 << 20;
     wide_norm_kernel<T, S><<<(unsigned)(a.n < most ? a.n : most), kThreads, 0, stream>>>(a);
     return hipGetLastError();

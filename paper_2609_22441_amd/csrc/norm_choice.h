@@ -14,10 +14,8 @@ struct NormShape {
 
 inline NormShape norm_shape(int32_t cols) {
     const int32_t blocks = (cols + 7) / 8;
-    if (blocks <= 16)
-        return {16, 1};
     if (blocks <= 64)
-        return {64, 1};
+        return {blocks <= 16 ? 16 : blocks <= 32 ? 32 : 64, 1};
     if (blocks <= 128)
         return {64, 2};
     if (blocks <= 256)
@@ -31,19 +29,38 @@ inline NormShape norm_shape(int32_t cols) {
     return {0, 0};
 }
 
-// The gradient's, which holds five matrices' elements and the sums over rows: one block a lane.
-inline int32_t norm_grad_lanes(int32_t cols) {
-    const int32_t blocks = (cols + 7) / 8;
-    return blocks <= 16 ? 16 : blocks <= 64 ? 64 : blocks <= 256 ? 256 : blocks <= 512 ? 512
-                                                                     : blocks <= 1024 ? 1024 : 0;
+// Workgroups of the norm for `rows` rows or groups of rows that a workgroup takes at a time: as many as the
+// chip holds, and of more rows one for each four, which keeps the chip full to the end (65,536 x 4,096 bf16
+// 484 us, with as many as it holds 558) and still reads the weights once for four rows.
+inline int64_t norm_groups(int64_t rows, int32_t threads) {
+    const int64_t held = 256 * (int64_t)(2048 / threads), fours = (rows + 3) / 4;
+    return rows < held ? rows : fours < held ? held : fours;
 }
 
-// Its workgroups, each of which adds up its rows: as many as the chip holds at a time.
+// The gradient's, which holds five matrices' elements and the sums over rows. Two blocks a lane where one
+// wavefront then has the row, without barriers (100,000 x 1,024 bf16 296 us, 321 in 128 lanes); of longer
+// rows one, which leaves room for more rows (65,536 x 4,096 804, 841 in 256 lanes).
+inline NormShape norm_grad_shape(int32_t cols) {
+    const int32_t blocks = (cols + 7) / 8;
+    if (blocks > 64 && blocks <= 128)
+        return {64, 2};
+    int32_t lanes = 16;
+    while (lanes < 1024 && lanes < blocks)
+        lanes *= 2;
+    return blocks <= lanes ? NormShape{lanes, 1} : NormShape{0, 0};
+}
+
+// Its workgroups, each of which adds up its rows to a partial result: as many as the chip holds at a time,
+// of fewer rows so many that each has eight, but not fewer than half of the chip holds (4,000 x 1,024 30 us
+// with as many as the chip holds, 20 with half of it; 1,000 x 2,048 24 and 17).
 inline int64_t norm_grad_groups(int64_t rows, int32_t cols) {
-    const int32_t lanes = norm_grad_lanes(cols), threads = lanes < 256 ? 256 : lanes;
-    const int64_t rows_at_once = threads / lanes, need = (rows + rows_at_once - 1) / rows_at_once;
+    const int32_t lanes = norm_grad_shape(cols).lanes, threads = lanes <= 64 ? 256 : lanes;
+    const int64_t at_once = threads / lanes, need = (rows + at_once - 1) / at_once;
     const int64_t most = 256 * (int64_t)(1024 / threads);
-    return need < most ? need : most;
+    const int64_t half = 256 * (int64_t)(threads < 512 ? 512 / threads : 1);
+    const int64_t eighth = (need + 7) / 8, some = need < half ? need : half;
+    const int64_t groups = eighth > some ? eighth : some;
+    return groups < most ? groups : most;
 }
 
 // Strips of rows whose sums over columns are partial results of one workgroup each, of the kernels that

@@ -16,177 +16,245 @@ struct RowStats {
 
 int64_t padded_cols(int32_t cols) { return ((int64_t)cols + kCols - 1) / kCols * kCols; }
 
-// The elements of a block and their gradients, in steps that need one more sum of the row each.
-template <typename T, typename S>
-struct Gradient : Forward<T, S> {
-    float yn[kCols], t[kCols], dy[kCols], v[kCols];
-    using Forward<T, S>::fn, Forward<T, S>::g, Forward<T, S>::y;
-    __device__ __forceinline__ void of_pre(const Raw<T> &dh, const float (&w)[kCols],
-                                           const RowNorm &pre) {
-#pragma unroll
-        for (int i = 0; i < kCols; ++i) {
-            yn[i] = (y[i] - pre.mean) * pre.r;
-            t[i] = (float)dh[i] * w[i];
-        }
-    }
-    // dy before post's weight: Y, and Y * scale.
-    __device__ __forceinline__ void of_sum(const NormGradArgs &a, const Raw<S> &d,
-                                           const RowStats &s) {
-#pragma unroll
-        for (int i = 0; i < kCols; ++i) {
-            dy[i] = (float)d[i];
-            if (a.dh)
-                dy[i] += a.a.pre == kNormNone ? t[i] : s.pre.r * (t[i] - s.t - yn[i] * s.t_yn);
-        }
-    }
-    __device__ __forceinline__ void of_post(const NormGradArgs &a, const float (&w)[kCols]) {
+// The gradient of a norm's input from that of its normalised value vn, of a block: 1 / its size r and the
+// row's means. Without a norm an infinity stays where it is.
+__device__ __forceinline__ void norm_back(int norm, const float (&t)[kCols], const float (&vn)[kCols],
+                                          float r, float mean_t, float mean_t_vn, float (&d)[kCols]) {
+    if (norm == kNormNone) {
 #pragma unroll
         for (int i = 0; i < kCols; ++i)
-            v[i] = dy[i] * a.a.scale * g[i] * w[i];
+            d[i] = t[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < kCols; ++i)
+            d[i] = r * (t[i] - mean_t - vn[i] * mean_t_vn);
     }
-};
+}
 
 // ---- rows in registers ----
 
-// L lanes of a row hold a block of 8 columns each, and for all the rows that they go through the weights of
-// their columns and the sums over rows. One read of f, gate, x, dy and dh, one write of dx, df and dgate;
-// four sums over the row's lanes one after another, two more with layer norms. At the end the groups of
-// lanes of a workgroup add up their sums in order. BIAS: with post's bias or the sums of either bias.
-// partial: [workgroups][kSums][padded columns].
-template <typename T, typename S, int L, bool TAIL, bool BIAS>
-__global__ __launch_bounds__(L < kThreads ? kThreads : L) void row_grad_kernel(NormGradArgs ga,
-                                                                               float *partial,
-                                                                               int64_t padded) {
+// L lanes of a row hold B blocks of 8 columns each, and for all the rows that they go through the sums over
+// rows of their columns. One read of f, gate, x, dy and dh, one write of dx, df and dgate; four sums over
+// the row's lanes one after another, two more with layer norms. Between these the vector units are what
+// is short (65,536 x 4,096 bf16: 750 instructions a lane and row were 55 % of their time at 1,226 us), so
+// that nothing is divided and no weight multiplied with scale for each row; and registers, of which a
+// wavefront may have 128 for four on a unit: what is behind one of the sums is computed again from the
+// elements as they were read, and vectors wait in LDS.
+// At the end the groups of lanes of a workgroup add up their sums in order. BIAS: with post's bias or the
+// sums of either bias. partial: [workgroups][kSums][padded columns].
+template <typename T, typename S, int L, int B, bool TAIL, bool BIAS>
+__global__ __launch_bounds__(L <= 64 ? kThreads : L, B == 2 ? 2 : BIAS ? 3 : 4) void row_grad_kernel(NormGradArgs ga,
+                                                                                  float *partial,
+                                                                                  int64_t padded) {
     const NormArgs &a = ga.a;
-    constexpr int kT = L < kThreads ? kThreads : L, kGroups = kT / L;
+    constexpr int kT = L <= 64 ? kThreads : L, kGroups = kT / L;
     constexpr int kV = BIAS ? kSums : 2;          // of Sum, the biases come last
-    __shared__ float place[2][L > 64 ? L / 64 : 1][2];
-    RowSum<L, 2> sum{place};
-    const int lane = threadIdx.x % L, col = lane * kCols, exchange = exchange_of(lane, a.cols);
-    const float cols = (float)a.cols;
-    float w[kCols], b[kCols] = {}, q[kCols], sums[kV][kCols] = {};
-    vector_block(a.post_weight, col, a.cols, 1.0f, w);
-    if (BIAS)
-        vector_block(a.post_bias, col, a.cols, 0.0f, b);
-    vector_block(a.pre_weight, col, a.cols, 1.0f, q);
-    auto in = [&](int e) { return col + (TAIL ? e : 0) < a.cols; };
-    for (int64_t row = (int64_t)blockIdx.x * kGroups + threadIdx.x / L; row < a.n;
+    __shared__ float place[2][2][L > 64 ? L / 64 : 1];
+    RowSum<L> sum{place};
+    const int lane = threadIdx.x % L;
+    const float per = 1.0f / (float)a.cols;
+    int col[B], exchange[B];
+    float w[B][kCols], sums[kV][B][kCols] = {};
+    // The vectors that a row's elements meet once or twice wait in LDS, where lanes' halves of a block lie
+    // side by side: pre's weight, post's bias.
+    typedef float four_t __attribute__((ext_vector_type(4)));
+    __shared__ __attribute__((aligned(16))) four_t waiting[BIAS ? 2 : 1][B][2][L];
+    auto vector = [&](int which, int i, float(&x)[kCols]) {
+        const four_t low = waiting[which][i][0][lane], high = waiting[which][i][1][lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            x[e] = low[e];
+            x[4 + e] = high[e];
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < B; ++i) {
+        col[i] = (lane + i * L) * kCols;
+        exchange[i] = exchange_of(lane + i * L, a.cols);
+        vector_block(a.post_weight, col[i], a.cols, 1.0f, w[i]);
+        times(w[i], a.scale);
+        if (threadIdx.x < L)
+#pragma unroll
+            for (int which = 0; which < (BIAS ? 2 : 1); ++which) {
+                float x[kCols];
+                vector_block(which ? a.post_bias : a.pre_weight, col[i], a.cols, which ? 0.0f : 1.0f, x);
+                times(x, which ? a.scale : 1.0f);
+                waiting[which][i][0][lane] = four_t{x[0], x[1], x[2], x[3]};
+                waiting[which][i][1][lane] = four_t{x[4], x[5], x[6], x[7]};
+            }
+    }
+    __syncthreads();
+    auto fetch = [&](auto &to, auto type, const void *p, int64_t stride, int64_t row) {
+        using E = decltype(type);
+#pragma unroll
+        for (int i = 0; i < B; ++i)
+            to[i] = p ? held_block<TAIL>(row_of<E>(p, stride, row), col[i], a.cols, exchange[i])
+                      : Raw<E>{};
+    };
+    for (int64_t row = (int64_t)blockIdx.x * kGroups + group_of_lanes<L>(); row < a.n;
          row += (int64_t)gridDim.x * kGroups) {
-        auto held = [&](auto type, const void *p, int64_t stride) {
-            using E = decltype(type);
-            return p ? held_block<TAIL>(row_of<E>(p, stride, row), col, a.cols, exchange) : Raw<E>{};
-        };
-        Raw<T> f = held(T(), a.f, a.f_stride), u = held(T(), a.gate, a.gate_stride);
-        Raw<S> x = held(S(), a.x, a.x_stride);
-        Raw<T> dh = held(T(), ga.dh, ga.dh_stride);
-        Raw<S> dy = held(S(), ga.dy, ga.dy_stride);
-        settle(f, exchange);
+        Raw<T> f[B], u[B], dh[B];
+        Raw<S> x[B], dy[B];
+        fetch(f, T(), a.f, a.f_stride, row);
+        fetch(u, T(), a.gate, a.gate_stride, row);
+        fetch(x, S(), a.x, a.x_stride, row);
+        fetch(dh, T(), ga.dh, ga.dh_stride, row);
+        fetch(dy, S(), ga.dy, ga.dy_stride, row);
+#pragma unroll
+        for (int i = 0; i < B; ++i)
+            settle(f[i], exchange[i]);
         RowStats st = {};
+        float v[B][kCols], g[B][kCols], slope[B][kCols], y[B][kCols];
+#pragma unroll
+        for (int i = 0; i < B; ++i)
+            numbers(f[i], v[i]);
+        st.post = norm_of<TAIL>(a.post, v, col, a.cols, per, a.post_eps, sum);
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+            settle(u[i], exchange[i]);
+            settle(x[i], exchange[i]);
+            settle(dh[i], exchange[i]);
+            settle(dy[i], exchange[i]);
+            float gate[kCols], stream[kCols], b[kCols] = {};
+            numbers(u[i], gate);
+            numbers(x[i], stream);
+            gate_block<true>(a.gate_kind, gate, g[i], slope[i]);
+            normalised(a.post, v[i], st.post, v[i]);
+            if (BIAS)
+                vector(1, i, b);
+            block_sum(stream, g[i], v[i], w[i], b, y[i]);
+        }
+        if (ga.dh) {
+            st.pre = norm_of<TAIL>(a.pre, y, col, a.cols, per, a.pre_eps, sum);
+            float s[2] = {};                      // of t * yn and t, which is 0 where the row has no column
+#pragma unroll
+            for (int i = 0; i < B; ++i) {
+                float d[kCols], yn[kCols], q[kCols];
+                vector(0, i, q);
+                numbers(dh[i], d);
+                normalised(a.pre, y[i], st.pre, yn);
+#pragma unroll
+                for (int e = 0; e < kCols; ++e) {
+                    s[0] += d[e] * q[e] * yn[e];
+                    sums[kPreWeight][i][e] += d[e] * yn[e];
+                    if (BIAS)
+                        sums[kPreBias][i][e] += d[e];
+                }
+                if (a.pre == kNormLayer)
+#pragma unroll
+                    for (int e = 0; e < kCols; ++e)
+                        s[1] += d[e] * q[e];
+#pragma unroll
+                for (int e = 0; e < kCols; ++e)
+                    again(y[i][e]);
+                again(dh[i]);
+            }
+            if (a.pre == kNormLayer) {
+                sum(s);
+                st.t = s[1] * per;
+                st.t_yn = s[0] * per;
+            } else if (a.pre == kNormRms) {
+                st.t_yn = sum(s[0]) * per;
+            }
+#pragma unroll
+            for (int i = 0; i < B; ++i) {
+                float d[kCols], t[kCols], yn[kCols], q[kCols];
+                vector(0, i, q);
+                numbers(dh[i], t);
+                numbers(dy[i], d);
+                normalised(a.pre, y[i], st.pre, yn);
+#pragma unroll
+                for (int e = 0; e < kCols; ++e)
+                    t[e] *= q[e];
+                norm_back(a.pre, t, yn, st.pre.r, st.t, st.t_yn, y[i]);
+#pragma unroll
+                for (int e = 0; e < kCols; ++e)
+                    y[i][e] += d[e];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < B; ++i)
+                numbers(dy[i], y[i]);
+        }
+        // y now holds the gradient of x.
+        float s[2] = {};
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+            if (ga.dx)
+                put_held<TAIL>(row_of<S>(ga.dx, ga.dx_stride, row), col[i], a.cols, exchange[i], y[i]);
+#pragma unroll
+            for (int e = 0; e < kCols; ++e) {
+                const float d = y[i][e] * g[i][e];
+                s[0] += d * w[i][e] * v[i][e];
+                sums[kPostWeight][i][e] += d * v[i][e];
+                if (BIAS)
+                    sums[kPostBias][i][e] += d;
+            }
+            if (a.post == kNormLayer)
+#pragma unroll
+                for (int e = 0; e < kCols; ++e)
+                    s[1] += y[i][e] * g[i][e] * w[i][e];
+#pragma unroll
+            for (int e = 0; e < kCols; ++e)
+                again(g[i][e]);
+        }
         if (a.post == kNormLayer) {
-            float s = 0.0f;
-#pragma unroll
-            for (int e = 0; e < kCols; ++e)
-                s += (float)f[e];
-            st.post.mean = sum(s) / cols;
-        }
-        if (a.post != kNormNone) {
-            float s = 0.0f;
-#pragma unroll
-            for (int e = 0; e < kCols; ++e) {
-                const float d = (float)f[e] - st.post.mean;
-                s += in(e) ? d * d : 0.0f;
-            }
-            st.post.r = inverse_size(sum(s), a.cols, a.post_eps);
-        }
-        settle(u, exchange);
-        settle(x, exchange);
-        Gradient<T, S> p;
-        p(a, f, u, x, st.post, w, b);
-        if (a.pre == kNormLayer) {
-            float s = 0.0f;
-#pragma unroll
-            for (int e = 0; e < kCols; ++e)
-                s += p.y[e];                      // 0 where the row has no column
-            st.pre.mean = sum(s) / cols;
-        }
-        if (a.pre != kNormNone) {
-            float s = 0.0f;
-#pragma unroll
-            for (int e = 0; e < kCols; ++e) {
-                const float d = p.y[e] - st.pre.mean;
-                s += in(e) ? d * d : 0.0f;
-            }
-            st.pre.r = inverse_size(sum(s), a.cols, a.pre_eps);
-        }
-        settle(dh, exchange);
-        settle(dy, exchange);
-        p.of_pre(dh, q, st.pre);
-        if (a.pre != kNormNone) {
-            float s[2] = {};
-#pragma unroll
-            for (int e = 0; e < kCols; ++e) {
-                s[0] += p.t[e];
-                s[1] += p.t[e] * p.yn[e];
-            }
             sum(s);
-            st.t = a.pre == kNormLayer ? s[0] / cols : 0.0f;
-            st.t_yn = s[1] / cols;
+            st.v = s[1] * per;
+            st.v_fn = s[0] * per;
+        } else if (a.post == kNormRms) {
+            st.v_fn = sum(s[0]) * per;
         }
-        p.of_sum(ga, dy, st);
-        p.of_post(ga, w);
-        if (a.post != kNormNone) {
-            float s[2] = {};
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+            float t[kCols], df[kCols], du[kCols], b[kCols] = {};
+            if (BIAS)
+                vector(1, i, b);
 #pragma unroll
             for (int e = 0; e < kCols; ++e) {
-                s[0] += p.v[e];
-                s[1] += p.v[e] * p.fn[e];
+                t[e] = y[i][e] * g[i][e] * w[i][e];
+                du[e] = y[i][e] * (v[i][e] * w[i][e] + b[e]) * slope[i][e];
             }
-            sum(s);
-            st.v = a.post == kNormLayer ? s[0] / cols : 0.0f;
-            st.v_fn = s[1] / cols;
+            norm_back(a.post, t, v[i], st.post.r, st.v, st.v_fn, df);
+            if (ga.dgate)
+                put_held<TAIL>(row_of<T>(ga.dgate, ga.dgate_stride, row), col[i], a.cols, exchange[i],
+                               du);
+            put_held<TAIL>(row_of<T>(ga.df, ga.df_stride, row), col[i], a.cols, exchange[i], df);
         }
-        float df[kCols], du[kCols];
+    }
 #pragma unroll
-        for (int e = 0; e < kCols; ++e) {
-            const float d = p.dy[e] * a.scale;
-            df[e] = a.post == kNormNone ? p.v[e] : st.post.r * (p.v[e] - st.v - p.fn[e] * st.v_fn);
-            du[e] = d * p.n[e] * p.slope[e];
-            sums[kPostWeight][e] += d * p.g[e] * p.fn[e];
-            sums[kPreWeight][e] += (float)dh[e] * p.yn[e];
-            if (BIAS) {
-                sums[kPostBias][e] += d * p.g[e];
-                sums[kPreBias][e] += (float)dh[e];
-            }
-        }
-        if (ga.dx)
-            put_held<TAIL>(row_of<S>(ga.dx, ga.dx_stride, row), col, a.cols, exchange, p.dy);
-        if (ga.dgate)
-            put_held<TAIL>(row_of<T>(ga.dgate, ga.dgate_stride, row), col, a.cols, exchange, du);
-        put_held<TAIL>(row_of<T>(ga.df, ga.df_stride, row), col, a.cols, exchange, df);
+    for (int i = 0; i < B; ++i) {
+        times(sums[kPostWeight][i], a.scale);
+        if (BIAS)
+            times(sums[kPostBias][i], a.scale);
     }
     if constexpr (kGroups == 1) {
-        if (col < a.cols)
 #pragma unroll
-            for (int v = 0; v < kV; ++v)
-                if (ga.sums[v])
-                    store_block(partial + ((int64_t)blockIdx.x * kSums + v) * padded + col, sums[v]);
+        for (int v = 0; v < kV; ++v)
+#pragma unroll
+            for (int i = 0; i < B; ++i)
+                if (ga.sums[v] && col[i] < a.cols)
+                    store_block(partial + ((int64_t)blockIdx.x * kSums + v) * padded + col[i],
+                                sums[v][i]);
     } else {
-        __shared__ float part[kGroups][L * kCols];
+        __shared__ float part[kGroups][B * L * kCols];
 #pragma unroll
         for (int v = 0; v < kV; ++v) {
             if (!ga.sums[v])
                 continue;
             __syncthreads();
 #pragma unroll
-            for (int e = 0; e < kCols; ++e)
-                part[threadIdx.x / L][col + e] = sums[v][e];
+            for (int i = 0; i < B; ++i)
+#pragma unroll
+                for (int e = 0; e < kCols; ++e)
+                    part[threadIdx.x / L][col[i] + e] = sums[v][i][e];
             __syncthreads();
-            for (int c = threadIdx.x; c < a.cols; c += kT) {
+            for (int at = threadIdx.x; at < a.cols; at += kT) {
                 float s = 0.0f;
 #pragma unroll
                 for (int g = 0; g < kGroups; ++g)
-                    s += part[g][c];
-                partial[((int64_t)blockIdx.x * kSums + v) * padded + c] = s;
+                    s += part[g][at];
+                partial[((int64_t)blockIdx.x * kSums + v) * padded + at] = s;
             }
         }
     }
@@ -194,112 +262,136 @@ __global__ __launch_bounds__(L < kThreads ? kThreads : L) void row_grad_kernel(N
 
 // ---- rows of any length ----
 
+// The elements of a block and their gradients, in steps that need one more sum of the row each.
+template <typename T, typename S>
+struct Gradient {
+    float w[kCols], b[kCols], q[kCols], fn[kCols], g[kCols], slope[kCols], y[kCols], yn[kCols], dh[kCols],
+        t[kCols], dy[kCols], v[kCols];
+    __device__ __forceinline__ void weights(const NormArgs &a, int col) {
+        vector_block(a.post_weight, col, a.cols, 1.0f, w);
+        vector_block(a.post_bias, col, a.cols, 0.0f, b);
+        vector_block(a.pre_weight, col, a.cols, 1.0f, q);
+        times(w, a.scale);
+        times(b, a.scale);
+    }
+    __device__ __forceinline__ void of_f(const NormArgs &a, int64_t row, int col) {
+        numbers(row_block(row_of<T>(a.f, a.f_stride, row), col, a.cols), fn);
+    }
+    __device__ __forceinline__ void of_block(const NormArgs &a, int64_t row, int col,
+                                             const RowNorm &post) {
+        float u[kCols], x[kCols];
+        of_f(a, row, col);
+        normalised(a.post, fn, post, fn);
+        numbers(a.gate ? row_block(row_of<T>(a.gate, a.gate_stride, row), col, a.cols) : Raw<T>{}, u);
+        numbers(a.x ? row_block(row_of<S>(a.x, a.x_stride, row), col, a.cols) : Raw<S>{}, x);
+        gate_block<true>(a.gate_kind, u, g, slope);
+        block_sum(x, g, fn, w, b, y);
+    }
+    __device__ __forceinline__ void of_pre(const NormGradArgs &ga, int64_t row, int col,
+                                           const RowNorm &pre) {
+        if (!ga.dh)
+            return;
+        numbers(row_block(row_of<T>(ga.dh, ga.dh_stride, row), col, ga.a.cols), dh);
+        normalised(ga.a.pre, y, pre, yn);
+#pragma unroll
+        for (int i = 0; i < kCols; ++i)
+            t[i] = dh[i] * q[i];
+    }
+    __device__ __forceinline__ void of_sum(const NormGradArgs &ga, int64_t row, int col,
+                                           const RowStats &s) {
+        float d[kCols];
+        numbers(ga.dy ? row_block(row_of<S>(ga.dy, ga.dy_stride, row), col, ga.a.cols) : Raw<S>{}, dy);
+        if (ga.dh) {
+            norm_back(ga.a.pre, t, yn, s.pre.r, s.t, s.t_yn, d);
+#pragma unroll
+            for (int i = 0; i < kCols; ++i)
+                dy[i] += d[i];
+        }
+#pragma unroll
+        for (int i = 0; i < kCols; ++i)
+            v[i] = dy[i] * g[i] * w[i];
+    }
+};
+
 // Each row's statistics, a workgroup a row: passes over the row as in the forward kernel, then one for
 // the sums of either norm's gradient.
 template <typename T, typename S>
 __global__ __launch_bounds__(kThreads) void wide_stats_kernel(NormGradArgs ga, RowStats *stats) {
     const NormArgs &a = ga.a;
-    __shared__ float place[2][kThreads / 64][2];
-    RowSum<kThreads, 2> sum{place};
+    __shared__ float place[2][2][kThreads / 64];
+    RowSum<kThreads> sum{place};
+    const float per = 1.0f / (float)a.cols;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
-        const T *f = row_of<T>(a.f, a.f_stride, row), *u = row_of<T>(a.gate, a.gate_stride, row);
-        const S *x = row_of<S>(a.x, a.x_stride, row), *dy = row_of<S>(ga.dy, ga.dy_stride, row);
-        const T *dh = row_of<T>(ga.dh, ga.dh_stride, row);
-        const float cols = (float)a.cols;
         auto over = [&](auto &&use) {
             for (int col = threadIdx.x * kCols; col < a.cols; col += kThreads * kCols)
                 use(col);
         };
         RowStats st = {};
+        Gradient<T, S> p;
+        float s[2] = {};
         if (a.post == kNormLayer) {
-            float s = 0.0f;
             over([&](int col) {
-                const Raw<T> v = row_block(f, col, a.cols);
-#pragma unroll
-                for (int i = 0; i < kCols; ++i)
-                    s += (float)v[i];
+                p.of_f(a, row, col);
+                s[0] += plain_sum(p.fn);
             });
-            st.post.mean = sum(s) / cols;
+            st.post.mean = sum(s[0]) * per;
         }
         if (a.post != kNormNone) {
-            float s = 0.0f;
+            s[0] = 0.0f;
             over([&](int col) {
-                const Raw<T> v = row_block(f, col, a.cols);
-#pragma unroll
-                for (int i = 0; i < kCols; ++i) {
-                    const float d = (float)v[i] - st.post.mean;
-                    s += col + i < a.cols ? d * d : 0.0f;
-                }
+                p.of_f(a, row, col);
+                s[0] += squares<true>(p.fn, st.post.mean, col, a.cols);
             });
-            st.post.r = inverse_size(sum(s), a.cols, a.post_eps);
+            st.post.r = inverse_size(sum(s[0]) * per, a.post_eps);
         }
-        Gradient<T, S> p;
-        float w[kCols], b[kCols];
         auto forward = [&](int col) {
-            vector_block(a.post_weight, col, a.cols, 1.0f, w);
-            vector_block(a.post_bias, col, a.cols, 0.0f, b);
-            p(a, row_block(f, col, a.cols), a.gate ? row_block(u, col, a.cols) : Raw<T>{},
-              a.x ? row_block(x, col, a.cols) : Raw<S>{}, st.post, w, b);
+            p.weights(a, col);
+            p.of_block(a, row, col, st.post);
         };
         if (a.pre == kNormLayer) {
-            float s = 0.0f;
+            s[0] = 0.0f;
             over([&](int col) {
-                forward(col);
-#pragma unroll
-                for (int i = 0; i < kCols; ++i)
-                    s += col + i < a.cols ? p.y[i] : 0.0f;
+                forward(col);                     // y is 0 where the row has no column
+                s[0] += plain_sum(p.y);
             });
-            st.pre.mean = sum(s) / cols;
+            st.pre.mean = sum(s[0]) * per;
         }
         if (a.pre != kNormNone) {
-            float s = 0.0f;
+            s[0] = 0.0f;
             over([&](int col) {
                 forward(col);
-#pragma unroll
-                for (int i = 0; i < kCols; ++i) {
-                    const float d = p.y[i] - st.pre.mean;
-                    s += col + i < a.cols ? d * d : 0.0f;
-                }
+                s[0] += squares<true>(p.y, st.pre.mean, col, a.cols);
             });
-            st.pre.r = inverse_size(sum(s), a.cols, a.pre_eps);
-        }
-        auto pre = [&](int col) {
-            forward(col);
-            if (ga.dh) {
-                float q[kCols];
-                vector_block(a.pre_weight, col, a.cols, 1.0f, q);
-                p.of_pre(row_block(dh, col, a.cols), q, st.pre);
-            }
-        };
-        if (a.pre != kNormNone) {
-            float s[2] = {};
+            st.pre.r = inverse_size(sum(s[0]) * per, a.pre_eps);
+            s[0] = s[1] = 0.0f;
             over([&](int col) {
-                pre(col);                         // dh, and with it t, is 0 behind the row's end
+                forward(col);
+                p.of_pre(ga, row, col, st.pre);
 #pragma unroll
                 for (int i = 0; i < kCols; ++i) {
-                    s[0] += p.t[i];
-                    s[1] += p.t[i] * (col + i < a.cols ? p.yn[i] : 0.0f);
+                    s[0] += p.t[i];               // 0 there, too
+                    s[1] += p.t[i] * p.yn[i];
                 }
             });
             sum(s);
-            st.t = a.pre == kNormLayer ? s[0] / cols : 0.0f;
-            st.t_yn = s[1] / cols;
+            st.t = a.pre == kNormLayer ? s[0] * per : 0.0f;
+            st.t_yn = s[1] * per;
         }
         if (a.post != kNormNone) {
-            float s[2] = {};
+            s[0] = s[1] = 0.0f;
             over([&](int col) {
-                pre(col);
-                p.of_sum(ga, ga.dy ? row_block(dy, col, a.cols) : Raw<S>{}, st);
-                p.of_post(ga, w);
+                forward(col);
+                p.of_pre(ga, row, col, st.pre);
+                p.of_sum(ga, row, col, st);
 #pragma unroll
                 for (int i = 0; i < kCols; ++i) {
-                    s[0] += col + i < a.cols ? p.v[i] : 0.0f;
-                    s[1] += col + i < a.cols ? p.v[i] * p.fn[i] : 0.0f;
+                    s[0] += p.v[i];
+                    s[1] += p.v[i] * p.fn[i];
                 }
             });
             sum(s);
-            st.v = a.post == kNormLayer ? s[0] / cols : 0.0f;
-            st.v_fn = s[1] / cols;
+            st.v = a.post == kNormLayer ? s[0] * per : 0.0f;
+            st.v_fn = s[1] * per;
         }
         if (threadIdx.x == 0)
             stats[row] = st;
@@ -317,44 +409,37 @@ __global__ __launch_bounds__(kThreads) void wide_grad_kernel(NormGradArgs ga, co
         return;
     const int col = (int)col64;
     const int64_t first = a.n * blockIdx.y / gridDim.y, end = a.n * (blockIdx.y + 1) / gridDim.y;
-    float w[kCols], b[kCols], q[kCols], sums[kSums][kCols] = {};
-    vector_block(a.post_weight, col, a.cols, 1.0f, w);
-    vector_block(a.post_bias, col, a.cols, 0.0f, b);
-    vector_block(a.pre_weight, col, a.cols, 1.0f, q);
+    float sums[kSums][kCols] = {};
+    Gradient<T, S> p;
+    p.weights(a, col);
     for (int64_t row = first; row < end; ++row) {
         const RowStats st = stats[row];
-        Gradient<T, S> p;
-        p(a, row_block(row_of<T>(a.f, a.f_stride, row), col, a.cols),
-          a.gate ? row_block(row_of<T>(a.gate, a.gate_stride, row), col, a.cols) : Raw<T>{},
-          a.x ? row_block(row_of<S>(a.x, a.x_stride, row), col, a.cols) : Raw<S>{}, st.post, w, b);
-        Raw<T> dh{};
-        if (ga.dh) {
-            dh = row_block(row_of<T>(ga.dh, ga.dh_stride, row), col, a.cols);
-            p.of_pre(dh, q, st.pre);
-        }
-        p.of_sum(ga, ga.dy ? row_block(row_of<S>(ga.dy, ga.dy_stride, row), col, a.cols) : Raw<S>{},
-                 st);
-        p.of_post(ga, w);
+        p.of_block(a, row, col, st.post);
+        p.of_pre(ga, row, col, st.pre);
+        p.of_sum(ga, row, col, st);
         float df[kCols], du[kCols];
 #pragma unroll
         for (int i = 0; i < kCols; ++i) {
-            const float d = p.dy[i] * a.scale;
-            df[i] = a.post == kNormNone ? p.v[i]
-                                        : st.post.r * (p.v[i] - st.v - p.fn[i] * st.v_fn);
-            du[i] = d * p.n[i] * p.slope[i];
-            sums[kPostWeight][i] += d * p.g[i] * p.fn[i];
-            sums[kPostBias][i] += d * p.g[i];
-            if (ga.dh) {
-                sums[kPreWeight][i] += (float)dh[i] * p.yn[i];
-                sums[kPreBias][i] += (float)dh[i];
-            }
+            const float dg = p.dy[i] * p.g[i];
+            du[i] = p.dy[i] * (p.fn[i] * p.w[i] + p.b[i]) * p.slope[i];
+            sums[kPostWeight][i] += dg * p.fn[i];
+            sums[kPostBias][i] += dg;
         }
+        norm_back(a.post, p.v, p.fn, st.post.r, st.v, st.v_fn, df);
+        if (ga.dh)
+#pragma unroll
+            for (int i = 0; i < kCols; ++i) {
+                sums[kPreWeight][i] += p.dh[i] * p.yn[i];
+                sums[kPreBias][i] += p.dh[i];
+            }
         if (ga.dx)
             put_block(row_of<S>(ga.dx, ga.dx_stride, row), col, a.cols, p.dy);
         if (ga.dgate)
             put_block(row_of<T>(ga.dgate, ga.dgate_stride, row), col, a.cols, du);
         put_block(row_of<T>(ga.df, ga.df_stride, row), col, a.cols, df);
     }
+    times(sums[kPostWeight], a.scale);
+    times(sums[kPostBias], a.scale);
 #pragma unroll
     for (int s = 0; s < kSums; ++s)
         if (ga.sums[s])
@@ -377,7 +462,7 @@ __global__ __launch_bounds__(64 * kFoldWaves) void fold_kernel(NormGradArgs ga, 
         return;                                   // all of the workgroup
     float sum = 0.0f;
     if (col < ga.a.cols)
-#pragma unroll 8
+#pragma unroll 16
         for (int64_t i = wave; i < strips; i += kFoldWaves)
             sum += partial[(i * kSums + s) * padded + col];
     part[wave][lane] = sum;
@@ -401,10 +486,10 @@ hipError_t fold(const NormGradArgs &g, const float *partial, int64_t strips, hip
     return hipGetLastError();
 }
 
-template <typename T, typename S, int L>
+template <typename T, typename S, int L, int B = 1>
 hipError_t launch_rows(const NormGradArgs &g, hipStream_t stream) {
     const NormArgs &a = g.a;
-    constexpr int kT = L < kThreads ? kThreads : L;
+    constexpr int kT = L <= 64 ? kThreads : L;
     const int64_t padded = padded_cols(a.cols), groups = norm_grad_groups(a.n, a.cols);
     float *partial = static_cast<float *>(g.workspace);
     auto even = [](const void *p, int64_t stride) { return !p || even_rows(p, stride); };
@@ -415,25 +500,28 @@ hipError_t launch_rows(const NormGradArgs &g, hipStream_t stream) {
     const bool bias = a.post_bias || g.sums[kPostBias] || g.sums[kPreBias];
     const unsigned grid = (unsigned)groups;
     if (tail && bias)
-        row_grad_kernel<T, S, L, true, true><<<grid, kT, 0, stream>>>(g, partial, padded);
+        row_grad_kernel<T, S, L, B, true, true><<<grid, kT, 0, stream>>>(g, partial, padded);
     else if (tail)
-        row_grad_kernel<T, S, L, true, false><<<grid, kT, 0, stream>>>(g, partial, padded);
+        row_grad_kernel<T, S, L, B, true, false><<<grid, kT, 0, stream>>>(g, partial, padded);
     else if (bias)
-        row_grad_kernel<T, S, L, false, true><<<grid, kT, 0, stream>>>(g, partial, padded);
+        row_grad_kernel<T, S, L, B, false, true><<<grid, kT, 0, stream>>>(g, partial, padded);
     else
-        row_grad_kernel<T, S, L, false, false><<<grid, kT, 0, stream>>>(g, partial, padded);
+        row_grad_kernel<T, S, L, B, false, false><<<grid, kT, 0, stream>>>(g, partial, padded);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? fold(g, partial, groups, stream) : e;
 }
 
 template <typename T, typename S>
 hipError_t launch_types(const NormGradArgs &g, hipStream_t stream) {
-    switch (norm_grad_lanes(g.a.cols)) {
-    case 16: return launch_rows<T, S, 16>(g, stream);
-    case 64: return launch_rows<T, S, 64>(g, stream);
-    case 256: return launch_rows<T, S, 256>(g, stream);
-    case 512: return launch_rows<T, S, 512>(g, stream);
-    case 1024: return launch_rows<T, S, 1024>(g, stream);
+    const NormShape shape = norm_grad_shape(g.a.cols);
+    switch (shape.lanes * 4 + shape.blocks) {
+    case 16 * 4 + 1: return launch_rows<T, S, 16>(g, stream);
+    case 32 * 4 + 1: return launch_rows<T, S, 32>(g, stream);
+    case 64 * 4 + 1: return launch_rows<T, S, 64>(g, stream);
+    case 256 * 4 + 1: return launch_rows<T, S, 256>(g, stream);
+    case 512 * 4 + 1: return launch_rows<T, S, 512>(g, stream);
+    case 1024 * 4 + 1: return launch_rows<T, S, 1024>(g, stream);
+    case 64 * 4 + 2: return launch_rows<T, S, 64, 2>(g, stream);
     }
     const int64_t padded = padded_cols(g.a.cols), strips = norm_wide_strips(g.a.n, g.a.cols);
     RowStats *stats = static_cast<RowStats *>(g.workspace);
@@ -452,7 +540,7 @@ hipError_t launch_types(const NormGradArgs &g, hipStream_t stream) {
 }  // namespace
 
 int64_t norm_grad_workspace_bytes(int64_t n, int32_t cols) {
-    if (norm_grad_lanes(cols))
+    if (norm_grad_shape(cols).lanes)
         return norm_grad_groups(n, cols) * kSums * padded_cols(cols) * 4;
     return n * (int64_t)sizeof(RowStats) + norm_wide_strips(n, cols) * kSums * padded_cols(cols) * 4;
 }

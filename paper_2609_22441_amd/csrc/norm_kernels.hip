@@ -8,36 +8,31 @@ namespace {
 constexpr int kThreads = 256;
 
 // Rows that stay in registers: L lanes of a row hold B blocks of 8 columns each, and weights and biases of
-// their columns for all the rows that they go through. One read of f, gate and x, one write of y and h;
-// the sums between them are over lanes, and over a workgroup's wavefronts through LDS.
-template <typename T, typename S, int L, int B, bool TAIL>
-__global__ __launch_bounds__(L < kThreads ? kThreads : L) void row_norm_kernel(NormArgs a) {
-    constexpr int kT = L < kThreads ? kThreads : L, kGroups = kT / L;
-    __shared__ float place[2][L > 64 ? L / 64 : 1][1];
-    RowSum<L, 1> sum{place};
+// their columns for all the rows that they go through. One read of f, gate and x, one write of y and h; the
+// sums between them are over lanes, and over a workgroup's wavefronts through LDS. BIAS: with either bias.
+template <typename T, typename S, int L, int B, bool TAIL, bool BIAS>
+__global__ __launch_bounds__(L <= 64 ? kThreads : L) void row_norm_kernel(NormArgs a) {
+    constexpr int kT = L <= 64 ? kThreads : L, kGroups = kT / L;
+    __shared__ float place[2][2][L > 64 ? L / 64 : 1];
+    RowSum<L> sum{place};
     const int lane = threadIdx.x % L;
+    const float per = 1.0f / (float)a.cols;
     int col[B], exchange[B];
-    float post_w[B][kCols], post_b[B][kCols], pre_w[B][kCols], pre_b[B][kCols];
+    float post_w[B][kCols], post_b[B][kCols] = {}, pre_w[B][kCols], pre_b[B][kCols] = {};
 #pragma unroll
     for (int i = 0; i < B; ++i) {
         col[i] = (lane + i * L) * kCols;
         exchange[i] = exchange_of(lane + i * L, a.cols);
         vector_block(a.post_weight, col[i], a.cols, 1.0f, post_w[i]);
-        vector_block(a.post_bias, col[i], a.cols, 0.0f, post_b[i]);
         vector_block(a.pre_weight, col[i], a.cols, 1.0f, pre_w[i]);
-        vector_block(a.pre_bias, col[i], a.cols, 0.0f, pre_b[i]);
+        if (BIAS) {
+            vector_block(a.post_bias, col[i], a.cols, 0.0f, post_b[i]);
+            vector_block(a.pre_bias, col[i], a.cols, 0.0f, pre_b[i]);
+        }
+        times(post_w[i], a.scale);
+        times(post_b[i], a.scale);
     }
-    // The sum over a row of use(block, element) where it has a column.
-    auto over = [&](auto &&use) {
-        float s = 0.0f;
-#pragma unroll
-        for (int i = 0; i < B; ++i)
-#pragma unroll
-            for (int e = 0; e < kCols; ++e)
-                s += col[i] + (TAIL ? e : 0) < a.cols ? use(i, e) : 0.0f;
-        return sum(s);
-    };
-    for (int64_t row = (int64_t)blockIdx.x * kGroups + threadIdx.x / L; row < a.n;
+    for (int64_t row = (int64_t)blockIdx.x * kGroups + group_of_lanes<L>(); row < a.n;
          row += (int64_t)gridDim.x * kGroups) {
         Raw<T> f[B], u[B];
         Raw<S> x[B];
@@ -55,39 +50,33 @@ __global__ __launch_bounds__(L < kThreads ? kThreads : L) void row_norm_kernel(N
 #pragma unroll
         for (int i = 0; i < B; ++i)
             settle(f[i], exchange[i]);
-        RowNorm post, pre;
-        if (a.post == kNormLayer)
-            post.mean = over([&](int i, int e) { return (float)f[i][e]; }) / (float)a.cols;
-        if (a.post != kNormNone)
-            post.r = inverse_size(over([&](int i, int e) {
-                                      const float d = (float)f[i][e] - post.mean;
-                                      return d * d;
-                                  }),
-                                  a.cols, a.post_eps);
-        Forward<T, S> p[B];
+        float v[B][kCols], y[B][kCols];
+#pragma unroll
+        for (int i = 0; i < B; ++i)
+            numbers(f[i], v[i]);
+        const RowNorm post = norm_of<TAIL>(a.post, v, col, a.cols, per, a.post_eps, sum);
 #pragma unroll
         for (int i = 0; i < B; ++i) {
             settle(u[i], exchange[i]);
             settle(x[i], exchange[i]);
-            p[i](a, f[i], u[i], x[i], post, post_w[i], post_b[i]);
-            put_held<TAIL>(row_of<S>(a.y, a.y_stride, row), col[i], a.cols, exchange[i], p[i].y);
+            float g[kCols], unused[kCols], gate[kCols], stream[kCols];
+            numbers(u[i], gate);
+            numbers(x[i], stream);
+            gate_block<false>(a.gate_kind, gate, g, unused);
+            normalised(a.post, v[i], post, v[i]);
+            block_sum(stream, g, v[i], post_w[i], post_b[i], y[i]);
+            put_held<TAIL>(row_of<S>(a.y, a.y_stride, row), col[i], a.cols, exchange[i], y[i]);
         }
         if (!a.h)
             continue;
-        if (a.pre == kNormLayer)
-            pre.mean = over([&](int i, int e) { return p[i].y[e]; }) / (float)a.cols;
-        if (a.pre != kNormNone)
-            pre.r = inverse_size(over([&](int i, int e) {
-                                     const float d = p[i].y[e] - pre.mean;
-                                     return d * d;
-                                 }),
-                                 a.cols, a.pre_eps);
+        const RowNorm pre = norm_of<TAIL>(a.pre, y, col, a.cols, per, a.pre_eps, sum);
 #pragma unroll
         for (int i = 0; i < B; ++i) {
             float h[kCols];
+            normalised(a.pre, y[i], pre, h);
 #pragma unroll
             for (int e = 0; e < kCols; ++e)
-                h[e] = (p[i].y[e] - pre.mean) * pre.r * pre_w[i][e] + pre_b[i][e];
+                h[e] = h[e] * pre_w[i][e] + pre_b[i][e];
             put_held<TAIL>(row_of<T>(a.h, a.h_stride, row), col[i], a.cols, exchange[i], h);
         }
     }
@@ -98,96 +87,91 @@ __global__ __launch_bounds__(L < kThreads ? kThreads : L) void row_norm_kernel(N
 // find the row in the caches.
 template <typename T, typename S>
 __global__ __launch_bounds__(kThreads) void wide_norm_kernel(NormArgs a) {
-    __shared__ float place[2][kThreads / 64][1];
-    RowSum<kThreads, 1> sum{place};
+    __shared__ float place[2][2][kThreads / 64];
+    RowSum<kThreads> sum{place};
+    const float per = 1.0f / (float)a.cols;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         const T *f = row_of<T>(a.f, a.f_stride, row), *u = row_of<T>(a.gate, a.gate_stride, row);
         const S *x = row_of<S>(a.x, a.x_stride, row);
+        // The sum over the row of use(col).
         auto over = [&](auto &&use) {
+            float s = 0.0f;
             for (int col = threadIdx.x * kCols; col < a.cols; col += kThreads * kCols)
-                use(col);
+                s += use(col);
+            return sum(s);
         };
+        auto block_f = [&](int col, float(&v)[kCols]) { numbers(row_block(f, col, a.cols), v); };
         RowNorm post, pre;
-        if (a.post == kNormLayer) {
-            float s = 0.0f;
-            over([&](int col) {
-                const Raw<T> v = row_block(f, col, a.cols);
-#pragma unroll
-                for (int i = 0; i < kCols; ++i)
-                    s += (float)v[i];
-            });
-            post.mean = sum(s) / (float)a.cols;
-        }
-        if (a.post != kNormNone) {
-            float s = 0.0f;
-            over([&](int col) {
-                const Raw<T> v = row_block(f, col, a.cols);
-#pragma unroll
-                for (int i = 0; i < kCols; ++i) {
-                    const float d = (float)v[i] - post.mean;
-                    s += col + i < a.cols ? d * d : 0.0f;
-                }
-            });
-            post.r = inverse_size(sum(s), a.cols, a.post_eps);
-        }
-        Forward<T, S> p;
+        if (a.post == kNormLayer)
+            post.mean = over([&](int col) {
+                            float v[kCols];
+                            block_f(col, v);
+                            return plain_sum(v);
+                        }) * per;
+        if (a.post != kNormNone)
+            post.r = inverse_size(over([&](int col) {
+                                      float v[kCols];
+                                      block_f(col, v);
+                                      return squares<true>(v, post.mean, col, a.cols);
+                                  }) * per,
+                                  a.post_eps);
+        float y[kCols];
         auto forward = [&](int col) {
-            float w[kCols], b[kCols];
+            float w[kCols], b[kCols], v[kCols], g[kCols], unused[kCols], gate[kCols], stream[kCols];
             vector_block(a.post_weight, col, a.cols, 1.0f, w);
             vector_block(a.post_bias, col, a.cols, 0.0f, b);
-            p(a, row_block(f, col, a.cols), a.gate ? row_block(u, col, a.cols) : Raw<T>{},
-              a.x ? row_block(x, col, a.cols) : Raw<S>{}, post, w, b);
+            times(w, a.scale);
+            times(b, a.scale);
+            block_f(col, v);
+            numbers(a.gate ? row_block(u, col, a.cols) : Raw<T>{}, gate);
+            numbers(a.x ? row_block(x, col, a.cols) : Raw<S>{}, stream);
+            gate_block<false>(a.gate_kind, gate, g, unused);
+            normalised(a.post, v, post, v);
+            block_sum(stream, g, v, w, b, y);
         };
-        if (a.pre == kNormLayer) {
-            float s = 0.0f;
-            over([&](int col) {
-                forward(col);
-#pragma unroll
-                for (int i = 0; i < kCols; ++i)
-                    s += col + i < a.cols ? p.y[i] : 0.0f;
-            });
-            pre.mean = sum(s) / (float)a.cols;
-        }
-        if (a.pre != kNormNone) {
-            float s = 0.0f;
-            over([&](int col) {
-                forward(col);
-#pragma unroll
-                for (int i = 0; i < kCols; ++i) {
-                    const float d = p.y[i] - pre.mean;
-                    s += col + i < a.cols ? d * d : 0.0f;
-                }
-            });
-            pre.r = inverse_size(sum(s), a.cols, a.pre_eps);
-        }
+        if (a.pre == kNormLayer)
+            pre.mean = over([&](int col) {
+                           forward(col);          // 0 where the row has no column
+                           return plain_sum(y);
+                       }) * per;
+        if (a.pre != kNormNone)
+            pre.r = inverse_size(over([&](int col) {
+                                     forward(col);
+                                     return squares<true>(y, pre.mean, col, a.cols);
+                                 }) * per,
+                                 a.pre_eps);
         over([&](int col) {
             forward(col);
-            put_block(row_of<S>(a.y, a.y_stride, row), col, a.cols, p.y);
+            put_block(row_of<S>(a.y, a.y_stride, row), col, a.cols, y);
             if (a.h) {
                 float w[kCols], b[kCols], h[kCols];
                 vector_block(a.pre_weight, col, a.cols, 1.0f, w);
                 vector_block(a.pre_bias, col, a.cols, 0.0f, b);
+                normalised(a.pre, y, pre, h);
 #pragma unroll
                 for (int i = 0; i < kCols; ++i)
-                    h[i] = (p.y[i] - pre.mean) * pre.r * w[i] + b[i];
+                    h[i] = h[i] * w[i] + b[i];
                 put_block(row_of<T>(a.h, a.h_stride, row), col, a.cols, h);
             }
+            return 0.0f;
         });
     }
 }
 
 template <typename T, typename S, int L, int B>
 hipError_t launch_rows(const NormArgs &a, hipStream_t stream) {
-    constexpr int kT = L < kThreads ? kThreads : L, kGroups = kT / L;
-    const int64_t groups = (a.n + kGroups - 1) / kGroups, most = 256 * (2048 / kT);
-    const unsigned grid = (unsigned)(groups < most ? groups : most);
+    constexpr int kT = L <= 64 ? kThreads : L, kGroups = kT / L;
+    const unsigned grid = (unsigned)norm_groups((a.n + kGroups - 1) / kGroups, kT);
+    const bool bias = a.post_bias || a.pre_bias;
     const bool even = a.cols % kCols == 0 && even_rows(a.f, a.f_stride) && even_rows(a.y, a.y_stride) &&
                       (!a.x || even_rows(a.x, a.x_stride)) && (!a.h || even_rows(a.h, a.h_stride)) &&
                       (!a.gate || even_rows(a.gate, a.gate_stride));
-    if (even)
-        row_norm_kernel<T, S, L, B, false><<<grid, kT, 0, stream>>>(a);
+    if (even && bias)
+        row_norm_kernel<T, S, L, B, false, true><<<grid, kT, 0, stream>>>(a);
+    else if (even)
+        row_norm_kernel<T, S, L, B, false, false><<<grid, kT, 0, stream>>>(a);
     else
-        row_norm_kernel<T, S, L, B, true><<<grid, kT, 0, stream>>>(a);
+        row_norm_kernel<T, S, L, B, true, true><<<grid, kT, 0, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -196,6 +180,7 @@ hipError_t launch_types(const NormArgs &a, hipStream_t stream) {
     const NormShape shape = norm_shape(a.cols);
     switch (shape.lanes * 4 + shape.blocks) {
     case 16 * 4 + 1: return launch_rows<T, S, 16, 1>(a, stream);
+    case 32 * 4 + 1: return launch_rows<T, S, 32, 1>(a, stream);
     case 64 * 4 + 1: return launch_rows<T, S, 64, 1>(a, stream);
     case 64 * 4 + 2: return launch_rows<T, S, 64, 2>(a, stream);
     case 256 * 4 + 1: return launch_rows<T, S, 256, 1>(a, stream);

@@ -51,11 +51,15 @@ class Bound:
         return Bound(v, self.e.sum(axis, keepdims=True) + roundings * F32 * size)
 
 
+def mean_of(s, cols):
+    """A sum times 1 / cols: the factor's rounding and the product's."""
+    return Bound(s.v / cols, s.e / cols + 2 * F32 * (np.abs(s.v) + s.e) / cols)
+
+
 def inverse_size(sum_, cols, eps):
-    """1 / sqrt(sum / cols + eps): quotient, sum, root and quotient, half a unit each; the root halves
-    its operand's relative error."""
-    eps32 = np.float64(np.float32(eps))
-    q = Bound(sum_.v / cols, sum_.e / cols + F32 * np.abs(sum_.v) / cols) + eps32
+    """1 / sqrt(sum / cols + eps): the root halves its operand's relative error, and is itself within a unit
+    in the last place."""
+    q = mean_of(sum_, cols) + np.float64(np.float32(eps))
     v = q.v ** -0.5
     low = np.maximum(q.v - q.e, q.v * 0.25)
     return Bound(v, v * (0.5 * q.e / low * (q.v / low) ** 0.5 + 2 * F32))
@@ -70,15 +74,14 @@ def unit(v, norm, eps):
         return v, Bound(1.0)
     if norm == LAYER:
         s = v.sum(1, roundings)
-        v = v - Bound(s.v / cols, s.e / cols + F32 * np.abs(s.v) / cols)
+        v = v - mean_of(s, cols)
     r = inverse_size((v * v).sum(1, roundings), cols, eps)
     return v * r, r
 
 
 def mean(v):
     cols = v.v.shape[1]
-    s = v.sum(1, 40 + cols // 256)
-    return Bound(s.v / cols, s.e / cols + F32 * np.abs(s.v) / cols)
+    return mean_of(v.sum(1, 40 + cols // 256), cols)
 
 
 def gate_of(u, kind):

@@ -84,9 +84,9 @@ def test_norm_grad_refuses():
                                        (9, 16_385), (2, 1 << 24), ((1 << 31) - 1, 16),
                                        ((1 << 31) - 1, 1 << 24)])
 def test_norm_grad_workspace_stays_small(rows, cols):
-    """Some hundred rows of sums, and of long rows 32 bytes each."""
+    """At most 2,048 rows of sums, and of long rows 32 bytes each."""
     size = Y.cc_block_norm_grad_workspace_bytes(rows, cols)
-    assert 0 < size <= 32 * rows + 16 * (cols + 8) * min(rows, 1024)
+    assert 0 < size <= 32 * rows + 16 * (cols + 8) * min(rows, 2048)
 
 
 def test_mxfp4_rows_refuse():

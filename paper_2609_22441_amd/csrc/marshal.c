@@ -57,7 +57,30 @@ typedef int (*linear_fn)(const void *, int64_t, int32_t, const int8_t *, int64_t
                          const float *, int64_t, int64_t, int64_t, int32_t, void *, int64_t, void *,
                          int64_t, void *);
 
+typedef int (*norm_fn)(const void *, int64_t, int32_t, const void *, int64_t, const void *, int64_t,
+                       int32_t, int32_t, int32_t, const float *, const float *, double, int32_t,
+                       const float *, const float *, double, double, int64_t, int32_t, void *,
+                       int64_t, void *, int64_t, void *);
+typedef int64_t (*norm_bytes_fn)(int64_t, int32_t);
+typedef int (*norm_grad_fn)(const void *, int64_t, int32_t, const void *, int64_t, const void *,
+                            int64_t, int32_t, int32_t, int32_t, const float *, const float *,
+                            double, int32_t, const float *, double, double, int64_t, int32_t,
+                            const void *, int64_t, const void *, int64_t, void *, int64_t, void *,
+                            int64_t, void *, int64_t, float *, float *, float *, float *, int32_t,
+                            void *, int64_t, void *);
+typedef int (*mx_quantize_fn)(const void *, int64_t, int32_t, int64_t, int32_t, uint8_t *, int64_t,
+                              uint8_t *, int64_t, void *);
+typedef int (*mx_dequantize_fn)(const uint8_t *, int64_t, const uint8_t *, int64_t, int64_t, int32_t,
+                                void *, int64_t, int32_t, void *);
+typedef int (*mx_matmul_fn)(const uint8_t *, int64_t, const uint8_t *, int64_t, const uint8_t *,
+                            int64_t, const uint8_t *, int64_t, const float *, int64_t, int64_t,
+                            int64_t, int32_t, void *, int64_t, int32_t, void *, int64_t, void *);
+typedef int (*mx_linear_fn)(const void *, int64_t, int32_t, const uint8_t *, int64_t,
+                            const uint8_t *, int64_t, const float *, int64_t, int64_t, int64_t,
+                            int32_t, void *, int64_t, void *, int64_t, void *);
+
 static PyObject *t_type, *t_i64, *t_i8;       /* torch.Tensor, torch.int64, torch.int8 */
+static PyObject *t_u8;                        /* torch.uint8 */
 static PyObject *t_float[3], *t_i32;          /* by type code: torch.float32, float16, bfloat16 */
 static PyObject *get_device, *raw_stream;     /* () -> current device; (device) -> its stream */
 static PyObject *n_get_device;
@@ -355,7 +378,7 @@ static PyObject *m_sort(PyObject *self, PyObject *const *a, Py_ssize_t n_args) {
 typedef struct {
     void *p;
     int64_t stride, rows, cols;               /* the row stride in bytes */
-    int32_t code;                             /* of the type: 0 to 2, or -1 for int8 */
+    int32_t code;                             /* of the type: 0 to 2, -1 for int8, -2 for uint8 */
 } Matrix;
 
 /* A tensor on device *device; the first one asked (*device < 0) says which. */
@@ -367,23 +390,25 @@ static int on_device(PyObject *x, int64_t *device) {
     return 1;
 }
 
-/* [rows, cols] with dense rows that do not overlap, of a floating-point type or (code -1) int8. */
+/* [rows, cols] with dense rows that do not overlap, of a floating-point type, or of 8 bits: int8 for 1,
+ * uint8 for 2. */
 static int matrix_of(PyObject *x, int eight_bits, int64_t *device, Matrix *m) {
-    static const int64_t size[] = {1, 4, 2, 2};
+    static const int64_t size[] = {1, 1, 4, 2, 2};
     int64_t step, inner;
     if (!plain(x, NULL))
         return 0;
     PyObject *d = PyObject_GetAttr(x, n_dtype);
     if (!d)
         return not_plain();
-    m->code = d == t_i8 ? -1 : d == t_float[0] ? 0 : d == t_float[1] ? 1 : d == t_float[2] ? 2 : 3;
+    m->code = d == t_i8 ? -1 : d == t_u8 ? -2 : d == t_float[0] ? 0 : d == t_float[1] ? 1
+              : d == t_float[2] ? 2 : 3;
     Py_DECREF(d);
-    if (m->code == 3 || (m->code < 0) != eight_bits ||
+    if (m->code == 3 || (m->code < 0 ? -m->code : 0) != eight_bits ||
         !pair_of(PyObject_GetAttr(x, n_shape), &m->rows, &m->cols) ||
         !pair_of(PyObject_CallMethodNoArgs(x, n_stride), &step, &inner) ||
         (inner != 1 && m->cols > 1) || (m->rows > 1 && step < m->cols) || !on_device(x, device))
         return 0;
-    m->stride = (m->rows > 1 ? step : m->cols) * size[m->code + 1];
+    m->stride = (m->rows > 1 ? step : m->cols) * size[m->code + 2];
     return m->cols <= INT32_MAX && pointer(x, &m->p);
 }
 
@@ -577,6 +602,185 @@ static PyObject *m_linear(PyObject *self, PyObject *const *a, Py_ssize_t n_args)
                          a[7] == Py_True, out.p, out.stride, ws, ws_bytes, stream));
 }
 
+static const Matrix no_matrix = {NULL, 0, 0, 0, 0};
+
+/* None, or [rows, cols] of the type of `code`. */
+static int optional_matrix(PyObject *x, int64_t rows, int64_t cols, int32_t code, int64_t *device,
+                           Matrix *m) {
+    *m = no_matrix;
+    return x == Py_None || (matrix_of(x, 0, device, m) && m->rows == rows && m->cols == cols &&
+                            m->code == code);
+}
+
+static int small(PyObject *x, int32_t *v) {
+    int64_t n;
+    if (!number(x, &n) || n != (int32_t)n)
+        return 0;
+    *v = (int32_t)n;
+    return 1;
+}
+
+/* norm(cc_block_norm, f, y, x, gate, gate_kind, post_norm, post_weight, post_bias, post_eps, scale, h,
+ * pre_norm, pre_weight, pre_bias, pre_eps, stream) */
+static PyObject *m_norm(PyObject *self, PyObject *const *a, Py_ssize_t n_args) {
+    (void)self;
+    void *fn, *stream, *w, *b, *q, *c;
+    Matrix f, y, x, gate, h;
+    int32_t kind, post, pre;
+    double post_eps, pre_eps, scale;
+    int64_t device = -1;
+    if (n_args != 17 || !address(a[0], &fn) || !matrix_of(a[1], 0, &device, &f) ||
+        !matrix_of(a[2], 0, &device, &y) || y.rows != f.rows || y.cols != f.cols ||
+        (y.code != f.code && y.code != 0) ||
+        !optional_matrix(a[3], f.rows, f.cols, y.code, &device, &x) ||
+        !optional_matrix(a[4], f.rows, f.cols, f.code, &device, &gate) || !small(a[5], &kind) ||
+        !small(a[6], &post) || !optional_vector(a[7], f.cols, &device, &w) ||
+        !optional_vector(a[8], f.cols, &device, &b) || !real(a[9], &post_eps) ||
+        !real(a[10], &scale) || !optional_matrix(a[11], f.rows, f.cols, f.code, &device, &h) ||
+        !small(a[12], &pre) || !optional_vector(a[13], f.cols, &device, &q) ||
+        !optional_vector(a[14], f.cols, &device, &c) || !real(a[15], &pre_eps) ||
+        !device_stream(a[16], device, &stream))
+        return no_call();
+    CALL(((norm_fn)fn)(x.p, x.stride, y.code, f.p, f.stride, gate.p, gate.stride, kind, f.code, post, w,
+                       b, post_eps, pre, q, c, pre_eps, scale, f.rows, (int32_t)f.cols, y.p, y.stride,
+                       h.p, h.stride, stream));
+}
+
+/* norm_grad(cc_block_norm_grad, cc_block_norm_grad_workspace_bytes, f, df, workspace, x, gate,
+ * gate_kind, post_norm, post_weight, post_bias, post_eps, scale, pre_norm, pre_weight, pre_bias,
+ * pre_eps, dy, dh, dx, dgate, d_post_weight, d_post_bias, d_pre_weight, d_pre_bias, accumulate,
+ * stream) */
+static PyObject *m_norm_grad(PyObject *self, PyObject *const *a, Py_ssize_t n_args) {
+    (void)self;
+    void *fn, *size, *stream, *ws, *w, *b, *q, *c, *sums[4];
+    Matrix f, df, x, gate, dy, dh, dx, dgate;
+    int32_t kind, post, pre, stream_code;
+    double post_eps, pre_eps, scale;
+    int64_t device = -1, ws_bytes;
+    if (n_args != 27 || !address(a[0], &fn) || !address(a[1], &size) ||
+        !matrix_of(a[2], 0, &device, &f))
+        return no_call();
+    /* The residual stream's type: that of dy, dx or x, whichever is given. */
+    PyObject *first = a[17] != Py_None ? a[17] : a[19] != Py_None ? a[19] : a[5];
+    stream_code = f.code;
+    if (first != Py_None) {
+        if (!matrix_of(first, 0, &device, &x) || (x.code != f.code && x.code != 0))
+            return no_call();
+        stream_code = x.code;
+    }
+    if ((a[17] == Py_None && a[18] == Py_None) || (a[20] != Py_None && a[6] == Py_None) ||
+        (a[18] == Py_None && (a[23] != Py_None || a[24] != Py_None)) || a[3] == Py_None ||
+        !optional_matrix(a[3], f.rows, f.cols, f.code, &device, &df) ||
+        !optional_matrix(a[5], f.rows, f.cols, stream_code, &device, &x) ||
+        !optional_matrix(a[6], f.rows, f.cols, f.code, &device, &gate) || !small(a[7], &kind) ||
+        !small(a[8], &post) || !optional_vector(a[9], f.cols, &device, &w) ||
+        !optional_vector(a[10], f.cols, &device, &b) || !real(a[11], &post_eps) ||
+        !real(a[12], &scale) || !small(a[13], &pre) || !optional_vector(a[14], f.cols, &device, &q) ||
+        !optional_vector(a[15], f.cols, &device, &c) || !real(a[16], &pre_eps) ||
+        !optional_matrix(a[17], f.rows, f.cols, stream_code, &device, &dy) ||
+        !optional_matrix(a[18], f.rows, f.cols, f.code, &device, &dh) ||
+        !optional_matrix(a[19], f.rows, f.cols, stream_code, &device, &dx) ||
+        !optional_matrix(a[20], f.rows, f.cols, f.code, &device, &dgate))
+        return no_call();
+    for (int i = 0; i < 4; ++i)
+        if (!optional_vector(a[21 + i], f.cols, &device, &sums[i]))
+            return no_call();
+    if ((a[25] != Py_True && a[25] != Py_False) ||
+        !workspace_of(a[4], ((norm_bytes_fn)size)(f.rows, (int32_t)f.cols), &device, &ws, &ws_bytes) ||
+        !device_stream(a[26], device, &stream))
+        return no_call();
+    CALL(((norm_grad_fn)fn)(x.p, x.stride, stream_code, f.p, f.stride, gate.p, gate.stride, kind,
+                            f.code, post, w, b, post_eps, pre, q, pre_eps, scale, f.rows,
+                            (int32_t)f.cols, dy.p, dy.stride, dh.p, dh.stride, dx.p, dx.stride,
+                            df.p, df.stride, dgate.p, dgate.stride, sums[0], sums[1], sums[2],
+                            sums[3], a[25] == Py_True, ws, ws_bytes, stream));
+}
+
+/* Rows of k values in 4 bits with their scales. */
+static int mx_of(PyObject *q, PyObject *scales, int64_t rows, int64_t k, int64_t *device, Matrix *m,
+                 Matrix *s) {
+    return matrix_of(q, 2, device, m) && matrix_of(scales, 2, device, s) && s->rows == m->rows &&
+           (rows < 0 || m->rows == rows) && m->cols == (k + 127) / 128 * 64 &&
+           s->cols == (k + 511) / 512 * 16;
+}
+
+/* mx_quantize(cc_quantize_mxfp4, x, q, scales, stream) */
+static PyObject *m_mx_quantize(PyObject *self, PyObject *const *a, Py_ssize_t n_args) {
+    (void)self;
+    void *fn, *stream;
+    Matrix x, q, s;
+    int64_t device = -1;
+    if (n_args != 5 || !address(a[0], &fn) || !matrix_of(a[1], 0, &device, &x) ||
+        !mx_of(a[2], a[3], x.rows, x.cols, &device, &q, &s) || !device_stream(a[4], device, &stream))
+        return no_call();
+    CALL(((mx_quantize_fn)fn)(x.p, x.stride, x.code, x.rows, (int32_t)x.cols, q.p, q.stride, s.p,
+                              s.stride, stream));
+}
+
+/* mx_dequantize(cc_dequantize_mxfp4, q, scales, out, stream) */
+static PyObject *m_mx_dequantize(PyObject *self, PyObject *const *a, Py_ssize_t n_args) {
+    (void)self;
+    void *fn, *stream;
+    Matrix out, q, s;
+    int64_t device = -1;
+    if (n_args != 5 || !address(a[0], &fn) || !matrix_of(a[3], 0, &device, &out) ||
+        !mx_of(a[1], a[2], out.rows, out.cols, &device, &q, &s) ||
+        !device_stream(a[4], device, &stream))
+        return no_call();
+    CALL(((mx_dequantize_fn)fn)(q.p, q.stride, s.p, s.stride, out.rows, (int32_t)out.cols, out.p,
+                                out.stride, out.code, stream));
+}
+
+/* mx_matmul(cc_matmul_mxfp4, cc_matmul_mxfp4_workspace_bytes, a, a_scales, b, b_scales, out, bias, relu,
+ * workspace, stream) */
+static PyObject *m_mx_matmul(PyObject *self, PyObject *const *a, Py_ssize_t n_args) {
+    (void)self;
+    void *fn, *size, *bias, *ws, *stream;
+    Matrix x, sx, w, sw, out;
+    int64_t ws_bytes, device = -1;
+    if (n_args != 11 || !address(a[0], &fn) || !address(a[1], &size) ||
+        !matrix_of(a[2], 2, &device, &x) || x.cols % 64 ||
+        !mx_of(a[2], a[3], -1, x.cols * 2, &device, &x, &sx) ||
+        !mx_of(a[4], a[5], -1, x.cols * 2, &device, &w, &sw) || !matrix_of(a[6], 0, &device, &out) ||
+        out.rows != x.rows || out.cols != w.rows ||
+        !optional_vector(a[7], w.rows, &device, &bias) || (a[8] != Py_True && a[8] != Py_False) ||
+        !workspace_of(a[9], ((product_bytes_fn)size)(x.rows, w.rows, x.cols * 2), &device, &ws,
+                      &ws_bytes) ||
+        !device_stream(a[10], device, &stream))
+        return no_call();
+    CALL(((mx_matmul_fn)fn)(x.p, x.stride, sx.p, sx.stride, w.p, w.stride, sw.p, sw.stride, bias,
+                            x.rows, w.rows, x.cols * 2, a[8] == Py_True, out.p, out.stride, out.code,
+                            ws, ws_bytes, stream));
+}
+
+/* mx_linear(cc_linear_mxfp4, cc_linear_mxfp4_workspace_bytes, x, w, w_scales, out, bias, relu, workspace,
+ * stream) */
+static PyObject *m_mx_linear(PyObject *self, PyObject *const *a, Py_ssize_t n_args) {
+    (void)self;
+    void *fn, *size, *bias, *ws, *stream;
+    Matrix x, w, sw, out;
+    int64_t ws_bytes, device = -1;
+    if (n_args != 10 || !address(a[0], &fn) || !address(a[1], &size) ||
+        !matrix_of(a[2], 0, &device, &x) || !mx_of(a[3], a[4], -1, x.cols, &device, &w, &sw) ||
+        !matrix_of(a[5], 0, &device, &out) || out.rows != x.rows || out.cols != w.rows ||
+        out.code != x.code || !optional_vector(a[6], w.rows, &device, &bias) ||
+        (a[7] != Py_True && a[7] != Py_False) ||
+        !workspace_of(a[8], ((product_bytes_fn)size)(x.rows, w.rows, x.cols), &device, &ws,
+                      &ws_bytes) ||
+        !device_stream(a[9], device, &stream))
+        return no_call();
+    CALL(((mx_linear_fn)fn)(x.p, x.stride, x.code, w.p, w.stride, sw.p, sw.stride, bias, x.rows, w.rows,
+                            x.cols, a[7] == Py_True, out.p, out.stride, ws, ws_bytes, stream));
+}
+
+/* init_blocks(torch.uint8) */
+static PyObject *m_init_blocks(PyObject *self, PyObject *u8) {
+    (void)self;
+    Py_INCREF(u8);
+    Py_XSETREF(t_u8, u8);
+    Py_RETURN_NONE;
+}
+
 /* init_layers(torch.float32, torch.float16, torch.bfloat16, torch.int32, get_device, raw_stream) */
 static PyObject *m_init_layers(PyObject *self, PyObject *args) {
     (void)self;
@@ -623,6 +827,13 @@ static PyMethodDef methods[] = {
     {"quantize", (PyCFunction)(void (*)(void))m_quantize, METH_FASTCALL, "cc_quantize_rows"},
     {"matmul", (PyCFunction)(void (*)(void))m_matmul, METH_FASTCALL, "cc_matmul_i8"},
     {"linear", (PyCFunction)(void (*)(void))m_linear, METH_FASTCALL, "cc_linear_i8"},
+    {"init_blocks", m_init_blocks, METH_O, "The type that the functions below need too."},
+    {"norm", (PyCFunction)(void (*)(void))m_norm, METH_FASTCALL, "cc_block_norm"},
+    {"norm_grad", (PyCFunction)(void (*)(void))m_norm_grad, METH_FASTCALL, "cc_block_norm_grad"},
+    {"mx_quantize", (PyCFunction)(void (*)(void))m_mx_quantize, METH_FASTCALL, "cc_quantize_mxfp4"},
+    {"mx_dequantize", (PyCFunction)(void (*)(void))m_mx_dequantize, METH_FASTCALL, "cc_dequantize_mxfp4"},
+    {"mx_matmul", (PyCFunction)(void (*)(void))m_mx_matmul, METH_FASTCALL, "cc_matmul_mxfp4"},
+    {"mx_linear", (PyCFunction)(void (*)(void))m_mx_linear, METH_FASTCALL, "cc_linear_mxfp4"},
     {NULL, NULL, 0, NULL}};
 
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal",

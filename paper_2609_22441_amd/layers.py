@@ -79,6 +79,7 @@ class _Layers:
             raw, device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
             L.marshal.init_layers(torch.float32, torch.float16, torch.bfloat16, torch.int32, device,
                                   raw)
+            L.marshal.init_blocks(torch.uint8)
             self.marshal = L.marshal
         except AttributeError:
             self.marshal = _b._ChecksOnly()
@@ -371,6 +372,10 @@ def cc_block_norm(f, y, x=None, gate=None, gate_kind: int = CC_GATE_SIGMOID,
     the residual sum, and the norm that the next block begins with. y and x are of f's type or float32,
     gate and h of f's; y may be x, h may be f (see include/cc_layers.h)."""
     L = _layers or _load()
+    st = L.marshal.norm(L.at_cc_block_norm, f, y, x, gate, gate_kind, post_norm, post_weight, post_bias,
+                        post_eps, scale, h, pre_norm, pre_weight, pre_bias, pre_eps, stream)
+    if st is not None:
+        return _check(st, "cc_block_norm")
     pf, f_stride, n, cols = _matrix(f, "f")
     t, ts = _type(L, f, "f"), _stream_type(L, y, f, "y")
     py, y_stride = _like(L, y, "y", y.dtype, n, cols, "y")
@@ -403,6 +408,13 @@ def cc_block_norm_grad(f, df, workspace, x=None, gate=None, gate_kind: int = CC_
     call's arguments are given again (pre_bias has no part in a gradient); dx may be dy, df may be
     dh. Equal calls give equal bits."""
     L = _layers or _load()
+    st = L.marshal.norm_grad(
+        L.at_cc_block_norm_grad, L.at_cc_block_norm_grad_workspace_bytes, f, df, workspace, x, gate,
+        gate_kind, post_norm, post_weight, post_bias, post_eps, scale, pre_norm, pre_weight, pre_bias,
+        pre_eps, dy, dh, dx, dgate, d_post_weight, d_post_bias, d_pre_weight, d_pre_bias, accumulate,
+        stream)
+    if st is not None:
+        return _check(st, "cc_block_norm_grad")
     pf, f_stride, n, cols = _matrix(f, "f")
     t = _type(L, f, "f")
     given = [(v, name) for v, name in ((dy, "dy"), (dx, "dx"), (x, "x")) if v is not None]
@@ -464,6 +476,9 @@ def cc_quantize_mxfp4(x, q, scales, stream=None) -> None:
     """q, scales: the rows of x in microscaled 4-bit floating point. q is uint8 [rows, 64 for each 128
     columns begun], two values to a byte; scales uint8 [rows, 16 for each 512 columns begun]."""
     L = _layers or _load()
+    st = L.marshal.mx_quantize(L.at_cc_quantize_mxfp4, x, q, scales, stream)
+    if st is not None:
+        return _check(st, "cc_quantize_mxfp4")
     px, x_stride, n, cols = _matrix(x, "x")
     t = _type(L, x, "x")
     pq, q_stride, ps, scales_stride, _, _ = _mx(L, q, scales, "q", cols, n)
@@ -475,6 +490,9 @@ def cc_quantize_mxfp4(x, q, scales, stream=None) -> None:
 def cc_dequantize_mxfp4(q, scales, out, stream=None) -> None:
     """out: the values of rows in 4 bits, as many columns as out has."""
     L = _layers or _load()
+    st = L.marshal.mx_dequantize(L.at_cc_dequantize_mxfp4, q, scales, out, stream)
+    if st is not None:
+        return _check(st, "cc_dequantize_mxfp4")
     po, out_stride, n, cols = _matrix(out, "out")
     t = _type(L, out, "out")
     pq, q_stride, ps, scales_stride, _, _ = _mx(L, q, scales, "q", cols, n)
@@ -492,6 +510,10 @@ def cc_matmul_mxfp4(a, a_scales, b, b_scales, out, bias=None, relu: bool = False
     """out = act(a b' + bias) for rows in 4 bits, a of m and b of n rows, as cc_quantize_mxfp4 writes
     them; sums are in 32 bits."""
     L = _layers or _load()
+    st = L.marshal.mx_matmul(L.at_cc_matmul_mxfp4, L.at_cc_matmul_mxfp4_workspace_bytes, a, a_scales, b,
+                             b_scales, out, bias, relu, workspace, stream)
+    if st is not None:
+        return _check(st, "cc_matmul_mxfp4")
     pa, a_stride, pas, as_stride, m, k = _mx(L, a, a_scales, "a")
     pb, b_stride, pbs, bs_stride, n, _ = _mx(L, b, b_scales, "b", k)
     pbias = _b._arr(bias, "bias", L.f32, n, optional=True)
@@ -515,6 +537,10 @@ def cc_linear_mxfp4(x, w, w_scales, out, bias=None, relu: bool = False, workspac
     """out = act(x W' + bias) with x put in 4 bits in the call and weights that cc_quantize_mxfp4 has put
     in 4 bits, one row per output."""
     L = _layers or _load()
+    st = L.marshal.mx_linear(L.at_cc_linear_mxfp4, L.at_cc_linear_mxfp4_workspace_bytes, x, w, w_scales,
+                             out, bias, relu, workspace, stream)
+    if st is not None:
+        return _check(st, "cc_linear_mxfp4")
     px, x_stride, m, k = _matrix(x, "x")
     t = _type(L, x, "x")
     pw, w_stride, pws, ws_stride, n, _ = _mx(L, w, w_scales, "w", k)

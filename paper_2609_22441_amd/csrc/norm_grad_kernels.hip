@@ -6,6 +6,7 @@ namespace ccj {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kWide = 1024;                        // of rows of any length
 
 // What the gradient of a row's elements needs of the whole row.
 struct RowStats {
@@ -316,14 +317,14 @@ struct Gradient {
 // Each row's statistics, a workgroup a row: passes over the row as in the forward kernel, then one for
 // the sums of either norm's gradient.
 template <typename T, typename S>
-__global__ __launch_bounds__(kThreads) void wide_stats_kernel(NormGradArgs ga, RowStats *stats) {
+__global__ __launch_bounds__(kWide) void wide_stats_kernel(NormGradArgs ga, RowStats *stats) {
     const NormArgs &a = ga.a;
-    __shared__ float place[2][2][kThreads / 64];
-    RowSum<kThreads> sum{place};
+    __shared__ float place[2][2][kWide / 64];
+    RowSum<kWide> sum{place};
     const float per = 1.0f / (float)a.cols;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         auto over = [&](auto &&use) {
-            for (int col = threadIdx.x * kCols; col < a.cols; col += kThreads * kCols)
+            for (int col = threadIdx.x * kCols; col < a.cols; col += kWide * kCols)
                 use(col);
         };
         RowStats st = {};
@@ -527,7 +528,7 @@ hipError_t launch_types(const NormGradArgs &g, hipStream_t stream) {
     RowStats *stats = static_cast<RowStats *>(g.workspace);
     float *partial = reinterpret_cast<float *>(stats + g.a.n);
     const int64_t most = 1 << 20;
-    wide_stats_kernel<T, S><<<(unsigned)(g.a.n < most ? g.a.n : most), kThreads, 0, stream>>>(g, stats);
+    wide_stats_kernel<T, S><<<(unsigned)(g.a.n < most ? g.a.n : most), kWide, 0, stream>>>(g, stats);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess)
         return e;

@@ -6,6 +6,7 @@ namespace ccj {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kWide = 1024;                        // of rows of any length
 
 // Rows that stay in registers: L lanes of a row hold B blocks of 8 columns each, and weights and biases of
 // their columns for all the rows that they go through. One read of f, gate and x, one write of y and h; the
@@ -86,9 +87,9 @@ __global__ __launch_bounds__(L <= 64 ? kThreads : L) void row_norm_kernel(NormAr
 // norm, a pass over x, f and the gate for each sum of y's, and one that writes. All but the first pass
 // find the row in the caches.
 template <typename T, typename S>
-__global__ __launch_bounds__(kThreads) void wide_norm_kernel(NormArgs a) {
-    __shared__ float place[2][2][kThreads / 64];
-    RowSum<kThreads> sum{place};
+__global__ __launch_bounds__(kWide) void wide_norm_kernel(NormArgs a) {
+    __shared__ float place[2][2][kWide / 64];
+    RowSum<kWide> sum{place};
     const float per = 1.0f / (float)a.cols;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         const T *f = row_of<T>(a.f, a.f_stride, row), *u = row_of<T>(a.gate, a.gate_stride, row);
@@ -96,7 +97,7 @@ __global__ __launch_bounds__(kThreads) void wide_norm_kernel(NormArgs a) {
         // The sum over the row of use(col).
         auto over = [&](auto &&use) {
             float s = 0.0f;
-            for (int col = threadIdx.x * kCols; col < a.cols; col += kThreads * kCols)
+            for (int col = threadIdx.x * kCols; col < a.cols; col += kWide * kCols)
                 s += use(col);
             return sum(s);
         };
@@ -189,7 +190,7 @@ hipError_t launch_types(const NormArgs &a, hipStream_t stream) {
     case 1024 * 4 + 2: return launch_rows<T, S, 1024, 2>(a, stream);
     }
     const int64_t most = 1 << 20;
-    wide_norm_kernel<T, S><<<(unsigned)(a.n < most ? a.n : most), kThreads, 0, stream>>>(a);
+    wide_norm_kernel<T, S><<<(unsigned)(a.n < most ? a.n : most), kWide, 0, stream>>>(a);
     return hipGetLastError();
 }
 

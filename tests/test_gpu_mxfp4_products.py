@@ -12,8 +12,7 @@ from layers_common import DEV, F32, HALF_ULP, TINY, TYPES, Output
 
 pytestmark = pytest.mark.gpu
 
-GRID = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6, 0, -0.5, -1, -1.5, -2, -3, -4, -6], dtype=torch.float64,
-                    device=DEV)
+GRID = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6, 0, -0.5, -1, -1.5, -2, -3, -4, -6], dtype=torch.float64)
 
 
 def gen(seed):
@@ -34,7 +33,7 @@ def four_bits(g, rows, k, pad=0):
 def values(q, s):
     codes = torch.stack([q & 15, q >> 4], 2).view(q.shape[0], -1).long()
     unit = torch.pow(2.0, s[:, :q.shape[1] // 16].double() - 127)
-    return GRID[codes] * unit.repeat_interleave(32, dim=1)
+    return GRID.to(DEV)[codes] * unit.repeat_interleave(32, dim=1)
 
 
 def check(o, want, size, steps, out, what):

@@ -92,15 +92,33 @@ __global__ __launch_bounds__(L <= 64 ? kThreads : L, B == 2 ? 2 : BIAS ? 3 : 4) 
             to[i] = p ? held_block<TAIL>(row_of<E>(p, stride, row), col[i], a.cols, exchange[i])
                       : Raw<E>{};
     };
-    for (int64_t row = (int64_t)blockIdx.x * kGroups + group_of_lanes<L>(); row < a.n;
-         row += (int64_t)gridDim.x * kGroups) {
+    struct Held {
         Raw<T> f[B], u[B], dh[B];
         Raw<S> x[B], dy[B];
-        fetch(f, T(), a.f, a.f_stride, row);
-        fetch(u, T(), a.gate, a.gate_stride, row);
-        fetch(x, S(), a.x, a.x_stride, row);
-        fetch(dh, T(), ga.dh, ga.dh_stride, row);
-        fetch(dy, S(), ga.dy, ga.dy_stride, row);
+    } next;
+    auto fetch_row = [&](int64_t row) {
+        fetch(next.f, T(), a.f, a.f_stride, row);
+        fetch(next.u, T(), a.gate, a.gate_stride, row);
+        fetch(next.x, S(), a.x, a.x_stride, row);
+        fetch(next.dh, T(), ga.dh, ga.dh_stride, row);
+        fetch(next.dy, S(), ga.dy, ga.dy_stride, row);
+    };
+    // Three wavefronts on a unit have registers for a row in 16 bits on its way while the row before is
+    // computed: layer norms of 50,000 x 512 bf16 94 us, 101 without; with a stream in 32 bits they have
+    // not (131,072 x 128 79 us, 167 with it), nor have four wavefronts.
+    constexpr bool kAhead = L <= 64 && B == 1 && BIAS && sizeof(S) == 2;
+    const int64_t step = (int64_t)gridDim.x * kGroups;
+    int64_t row = (int64_t)blockIdx.x * kGroups + group_of_lanes<L>();
+    if (kAhead && row < a.n)
+        fetch_row(row);
+    for (; row < a.n; row += step) {
+        if (!kAhead)
+            fetch_row(row);
+        Held held = next;
+        auto &f = held.f, &u = held.u, &dh = held.dh;
+        auto &x = held.x, &dy = held.dy;
+        if (kAhead && row + step < a.n)
+            fetch_row(row + step);
 #pragma unroll
         for (int i = 0; i < B; ++i)
             settle(f[i], exchange[i]);

@@ -1,4 +1,7 @@
 // Gradients of the norms around a block, its gate and its residual sum.
+//
+// 65,536 x 4,096 bf16 with gate, residual and both norms 800 us (4.29 GB at 5.4 TB/s; in pieces through the
+// caches 1,999), 50,000 x 512 bf16, a layer norm alone, 49 (two launches; 154 MB at 3.4 TB/s).
 #include "norm_choice.h"
 #include "norm_device.h"
 
@@ -44,9 +47,8 @@ __device__ __forceinline__ void norm_back(int norm, const float (&t)[kCols], con
 // At the end the groups of lanes of a workgroup add up their sums in order. BIAS: with post's bias or the
 // sums of either bias. partial: [workgroups][kSums][padded columns].
 template <typename T, typename S, int L, int B, bool TAIL, bool BIAS>
-__global__ __launch_bounds__(L <= 64 ? kThreads : L, B == 2 ? 2 : BIAS ? 3 : 4) void row_grad_kernel(NormGradArgs ga,
-                                                                                  float *partial,
-                                                                                  int64_t padded) {
+__global__ __launch_bounds__(L <= 64 ? kThreads : L, B == 2 ? 2 : BIAS ? 3 : 4) void row_grad_kernel(
+    NormGradArgs ga, float *partial, int64_t padded) {
     const NormArgs &a = ga.a;
     constexpr int kT = L <= 64 ? kThreads : L, kGroups = kT / L;
     constexpr int kV = BIAS ? kSums : 2;          // of Sum, the biases come last

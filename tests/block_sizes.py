@@ -15,5 +15,6 @@ PRODUCTS = [
 ]
 
 # Linear layers whose rows the skinny kernel puts in 4 bits itself, and some just past its limits.
-INSIDE = [(1, 500, 32_768), (16, 640, 2_048), (13, 555, 2_400), (1, 16_384, 4_096), (7, 300, 4_600), (2, 9_000, 99)]
+INSIDE = [(1, 500, 32_768), (16, 640, 2_048), (13, 555, 2_400), (1, 16_384, 4_096), (7, 300, 4_600),
+          (2, 9_000, 99)]
 OUTSIDE = [(1, 500, 32_769), (16, 640, 2_049), (1, 16_400, 96), (17, 64, 96), (16, 4_097, 2_048)]

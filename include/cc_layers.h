@@ -229,7 +229,7 @@ CC_API cc_status cc_linear_i8(const void *x, int64_t x_stride, int32_t type, con
  *   type        of f, gate and h; stream_type: of x and y, which is `type` or CC_F32.
  *   post_norm, pre_norm    CC_NORM_*; pre_* is ignored without h.
  *   *_weight, *_bias       [cols] float, or NULL.
- *   *_eps       ignored for CC_NORM_NONE; else positive and finite in 32 bits.
+ *   *_eps       ignored for CC_NORM_NONE; else from 2^-126 up and finite in 32 bits.
  *   scale       finite; rounded to 32 bits.
  *   n_rows      below 2^31; cols: 1 to 2^24.
  *   y           [n_rows][cols] of stream_type; h: [n_rows][cols] of `type`, or NULL.

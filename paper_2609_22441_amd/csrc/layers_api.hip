@@ -101,10 +101,10 @@ bool apart(const Span &out, std::initializer_list<Span> others) {
 
 bool norm_known(int32_t norm) { return norm >= CC_NORM_NONE && norm <= CC_NORM_LAYER; }
 
-// A norm's eps in 32 bits.
+// A norm's eps in 32 bits, whose inverse root the kernels take: not a subnormal number.
 bool eps_ok(int32_t norm, double eps, float *to) {
     *to = norm == CC_NORM_NONE ? 1.0f : (float)eps;
-    return *to > 0.0f && *to < INFINITY;
+    return *to >= 0x1p-126f && *to < INFINITY;
 }
 
 // The arguments that the norm and its gradient share, and what x, f and gate span.

@@ -31,10 +31,11 @@ inline NormShape norm_shape(int32_t cols) {
 
 // Workgroups of the norm for `rows` rows or groups of rows that a workgroup takes at a time: as many as the
 // chip holds, and of more rows one for each four, which keeps the chip full to the end (65,536 x 4,096 bf16
-// 484 us, with as many as it holds 558) and still reads the weights once for four rows.
+// 484 us, with as many as it holds 558) and still reads the weights once for four rows; a launch may not have
+// any number of them.
 inline int64_t norm_groups(int64_t rows, int32_t threads) {
-    const int64_t held = 256 * (int64_t)(2048 / threads), fours = (rows + 3) / 4;
-    return rows < held ? rows : fours < held ? held : fours;
+    const int64_t held = 256 * (int64_t)(2048 / threads), fours = (rows + 3) / 4, most = 1 << 20;
+    return rows < held ? rows : fours < held ? held : fours < most ? fours : most;
 }
 
 // The gradient's, which holds five matrices' elements and the sums over rows. Two blocks a lane where one

@@ -1,5 +1,6 @@
-"""The choice of kernels of the 4-bit products (csrc/mx_choice.h, compiled for the host): every kernel is
-reached, sizes at the rule's edges, and the GPU tests' sizes among them."""
+"""The choice of kernels of the 4-bit products (csrc/mx_choice.h) and of the block norms
+(csrc/norm_choice.h), compiled for the host: every kernel is reached, sizes at the rule's edges, and the GPU
+tests' sizes among them."""
 from __future__ import annotations
 
 import ctypes
@@ -9,11 +10,20 @@ from pathlib import Path
 
 import pytest
 
-from block_sizes import INSIDE, OUTSIDE, PRODUCTS, SKINNY, TILE64, TILE128, TILE256
+from block_sizes import (INSIDE, MANY_ROWS, NORMS, OUTSIDE, PRODUCTS, SKINNY, TILE64, TILE128,
+                         TILE256)
 
 CSRC = Path(__file__).resolve().parent.parent / "paper_2609_22441_amd" / "csrc"
 
 SHIM = """#include "mx_choice.h"
+#include "norm_choice.h"
+extern "C" int norm(int32_t cols) { return ccj::norm_shape(cols).lanes * 4 + ccj::norm_shape(cols).blocks; }
+extern "C" int grad(int32_t cols) {
+    return ccj::norm_grad_shape(cols).lanes * 4 + ccj::norm_grad_shape(cols).blocks;
+}
+extern "C" int64_t groups(int64_t rows, int32_t threads) { return ccj::norm_groups(rows, threads); }
+extern "C" int64_t grad_groups(int64_t rows, int32_t cols) { return ccj::norm_grad_groups(rows, cols); }
+extern "C" int64_t strips(int64_t rows, int32_t cols) { return ccj::norm_wide_strips(rows, cols); }
 extern "C" int product(int64_t m, int64_t n, int64_t k) { return ccj::mx_product_choice(m, n, k); }
 extern "C" int inside(int64_t m, int64_t n, int64_t k) { return ccj::mx_quantize_inside(m, n, k); }
 extern "C" int64_t lds(int64_t m, int64_t k) { return ccj::mx_quantize_lds(m, k); }
@@ -35,6 +45,9 @@ def choice():
     for name in ("product", "inside"):
         getattr(lib, name).argtypes = [ctypes.c_int64] * 3
     lib.lds.argtypes, lib.lds.restype = [ctypes.c_int64] * 2, ctypes.c_int64
+    for name in ("groups", "grad_groups", "strips"):
+        f = getattr(lib, name)
+        f.argtypes, f.restype = [ctypes.c_int64, ctypes.c_int32], ctypes.c_int64
     return lib
 
 
@@ -67,3 +80,39 @@ def test_quantised_rows_fit_in_lds(choice):
     for m in range(1, 17):
         k = 32_768 // m // 128 * 128
         assert choice.inside(m, 16, k) and choice.lds(m, k) <= 48 << 10
+
+
+def shapes(of):
+    return {divmod(of(cols), 4) for cols in range(1, 20_000)}
+
+
+def test_norm_shapes_hold_their_rows(choice):
+    """A row's lanes hold all of its blocks, and no fewer lanes of the same kernel would."""
+    for cols in list(range(1, 16_385)) + [16_385, 1 << 24]:
+        for of, most in ((choice.norm, 16_384), (choice.grad, 8_192)):
+            lanes, blocks = divmod(of(cols), 4)
+            assert (lanes == 0) == (cols > most)
+            assert lanes == 0 or lanes * blocks * 8 >= cols
+
+
+def test_the_gpu_tests_reach_every_norm_kernel(choice):
+    """Of each kernel, rows of whole blocks and others; and more rows than a launch goes through at once."""
+    for of in (choice.norm, choice.grad):
+        for even in (True, False):
+            assert {divmod(of(cols), 4) for _, cols in NORMS if (cols % 8 == 0) == even} == shapes(of)
+    for rows, cols in MANY_ROWS:
+        lanes = choice.grad(cols) // 4
+        threads = 256 if lanes <= 64 else lanes
+        assert rows > 2 * choice.grad_groups(rows, cols) * (threads // lanes)
+    assert {choice.grad(cols) // 4 for _, cols in MANY_ROWS} >= {16, 32, 64, 256, 512, 1024}
+
+
+def test_norm_launches_are_of_a_launchs_size(choice):
+    for rows in (1, 2, 3, 4, 2_047, 2_048, 10_000, 1 << 20, (1 << 31) - 1):
+        for threads in (256, 512, 1_024):
+            n = choice.groups(rows, threads)
+            assert 1 <= n <= rows and n * threads < 1 << 32
+        for cols in (1, 100, 1_000, 2_000, 4_000, 8_000):
+            assert 1 <= choice.grad_groups(rows, cols) <= min(rows, 1_024)
+        for cols in (9_000, 20_000, 1 << 24):
+            assert 1 <= choice.strips(rows, cols) <= min(rows, 2_048)

@@ -7,6 +7,7 @@ import pytest
 import torch
 
 import block_oracle as O
+from block_sizes import MANY_ROWS, NORMS
 import paper_2609_22441_amd as P
 from gpu_common import note
 from layers_common import DEV, HALF_ULP, TINY, TYPES, Output, assert_close, on_gpu, rng, values
@@ -91,15 +92,7 @@ def check_grad(c, t, dtype, stream, r, pre=True, with_dy=True, pad=0, shift=0, s
 
 TYPE_PAIRS = [("bf16", "bf16"), ("bf16", "f32"), ("f16", "f16"), ("f16", "f32"), ("f32", "f32")]
 
-# One column; part of a block of 8; rows for 16 lanes, a wavefront, workgroups of 256 to 1,024; odd
-# ends in each; rows in pieces.
-SIZES = [(1, 1), (3, 2), (5, 7), (70, 8), (33, 97), (40, 128), (37, 136), (21, 256), (19, 300),
-         (18, 512), (9, 520), (11, 1_003), (7, 1_024), (5, 1_032), (6, 2_048), (5, 2_051),
-         (4, 4_096), (3, 4_104), (3, 8_192), (2, 9_001), (2, 16_384), (2, 16_392), (3, 20_003),
-         (2, 40_000)]
-
-
-@pytest.mark.parametrize("rows,cols", SIZES)
+@pytest.mark.parametrize("rows,cols", NORMS)
 def test_sizes(rows, cols):
     note(f"block norm {rows}x{cols}")
     for i, (dtype, stream) in enumerate(TYPE_PAIRS):
@@ -146,14 +139,55 @@ def test_strides_and_alignment(dtype, stream, pad, shift):
         check_grad(c, t, dtype, stream, r, pad=pad, shift=shift)
 
 
-@pytest.mark.parametrize("rows,cols", [(5_000, 96), (3_001, 520), (1_100, 2_048), (700, 4_096)])
-def test_many_rows(rows, cols):
+@pytest.mark.parametrize("rows,cols", NORMS)
+def test_without_biases(rows, cols):
+    """Instantiations of their own."""
+    note(f"block norm without biases {rows}x{cols}")
+    for i, (dtype, stream) in enumerate(TYPE_PAIRS):
+        r = rng(cols * 10 + 5 + i)
+        c, t = make(r, rows, cols, dtype, stream, post=O.RMS if i % 2 else O.LAYER,
+                    weights=("post_weight", "pre_weight"))
+        check_forward(c, t, dtype, stream, True)
+        check_grad(c, t, dtype, stream, r, sums=("post_weight", "pre_weight"))
+
+
+@pytest.mark.parametrize("rows,cols", MANY_ROWS)
+@pytest.mark.parametrize("weights", [VECTORS, ("post_weight", "pre_weight")])
+def test_many_rows(rows, cols, weights):
     """More rows than a launch has groups of lanes."""
     note(f"block norm many rows {rows}x{cols}")
     r = rng(rows)
-    c, t = make(r, rows, cols, post=O.LAYER)
+    c, t = make(r, rows, cols, post=O.LAYER, weights=weights)
     check_forward(c, t, "bf16", "bf16", True)
-    check_grad(c, t, "bf16", "bf16", r)
+    check_grad(c, t, "bf16", "bf16", r, sums=weights)
+
+
+def test_offsets_past_32_bits():
+    """Rows 2^23 bytes apart, the last ones beyond 4 GiB: the same bits as of dense rows."""
+    note("block norm far rows")
+    rows, step = 520, (1 << 22) + 8
+    for cols in (104, 2_048, 17_000):
+        r = rng(cols)
+        c, t = make(r, rows, cols, "bf16", "bf16", post=O.LAYER)
+        moved = {k: v.to(DEV) for k, v in t.items()}
+        f = moved.pop("f")
+        wide = torch.empty((rows - 1) * step + cols, dtype=torch.bfloat16, device=DEV)
+        far = wide.as_strided((rows, cols), (step, 1))
+        y, h, far_h = torch.empty_like(f), torch.empty_like(f), torch.empty_like(f)
+        P.cc_block_norm(f, y, h=h, **moved, **options(c))
+        far.copy_(f)
+        P.cc_block_norm(far, y, h=far_h, **moved, **options(c))
+        assert torch.equal(h, far_h)
+        P.cc_block_norm(f, far, h=far_h, **moved, **options(c))
+        assert torch.equal(far, y)
+        ws = torch.empty(P.cc_block_norm_grad_workspace_bytes(rows, cols), dtype=torch.uint8, device=DEV)
+        dh, df, far_df = torch.randn_like(f), torch.empty_like(f), torch.empty_like(f)
+        P.cc_block_norm_grad(f, df, ws, dh=dh, **moved, **options(c))
+        far.copy_(f)
+        P.cc_block_norm_grad(far, far_df, ws, dh=dh, **moved, **options(c))
+        assert torch.equal(df, far_df)
+        P.cc_block_norm_grad(f, far, ws, dh=dh, **moved, **options(c))
+        assert torch.equal(df, far)
 
 
 def test_rows_far_from_zero():

@@ -69,6 +69,17 @@ def test_product(m, n, k, kernel):
         check(o, want, size, -(-k // 64), out, f"{m}x{n}x{k} {out}")
 
 
+@pytest.mark.parametrize("m,n", [(3, 5), (300, 300), (2_100, 1_281), (3_000, 3_001)])
+def test_products_of_no_columns(m, n):
+    """k = 0: the bias, by every kernel."""
+    note(f"mxfp4 product {m}x{n}x0")
+    none = [torch.empty(rows, 0, dtype=torch.uint8, device=DEV) for rows in (m, n)]
+    bias = torch.randn(n, device=DEV)
+    out = torch.full((m, n), 7.0, device=DEV)
+    P.cc_matmul_mxfp4(none[0], none[0], none[1], none[1], out, bias=bias)
+    assert torch.equal(out, bias.expand(m, n))
+
+
 @pytest.mark.parametrize("m,n,k,kernel", [p for p in PRODUCTS if p[0] * p[1] < 12_000_000])
 def test_equal_calls_give_equal_bits(m, n, k, kernel):
     note(f"mxfp4 product again {m}x{n}x{k}")

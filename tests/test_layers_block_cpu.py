@@ -26,7 +26,7 @@ NORM_REFUSALS = [
     dict(type=-1), dict(stream_type=1), dict(stream_type=4), dict(type=0, stream_type=2),
     dict(post=3), dict(post=-1), dict(pre=3), dict(gate_kind=2), dict(gate_kind=-1),
     dict(post_eps=0.0), dict(post_eps=-1.0), dict(post_eps=NAN), dict(post_eps=INF),
-    dict(post_eps=1e-60), dict(post_eps=1e39), dict(pre_eps=0.0), dict(scale=NAN), dict(scale=INF),
+    dict(post_eps=1e-60), dict(post_eps=1e-38), dict(pre_eps=1e-40), dict(post_eps=1e39), dict(pre_eps=0.0), dict(scale=NAN), dict(scale=INF),
     dict(scale=1e39), dict(post_weight=0x400002), dict(post_bias=0x410001),
     dict(pre_weight=0x420003), dict(x=0x100002), dict(x_stride=126), dict(x_stride=130),
     dict(f=None), dict(f=0x200001), dict(f_stride=62), dict(f_stride=65), dict(gate=0x300001),

@@ -38,15 +38,18 @@ inline int64_t norm_groups(int64_t rows, int32_t threads) {
     return rows < held ? rows : fours < held ? held : fours < most ? fours : most;
 }
 
-// The gradient's, which holds five matrices' elements and the sums over rows. Two blocks a lane where one
-// wavefront then has the row, without barriers (100,000 x 1,024 bf16 296 us, 321 in 128 lanes); of longer
-// rows one, which leaves room for more rows (65,536 x 4,096 804, 841 in 256 lanes).
-inline NormShape norm_grad_shape(int32_t cols) {
+// The gradient's, which holds five matrices' elements and the sums over rows; wide: the residual stream is in
+// 32 bits, which leaves fewer registers. Two blocks a lane where one wavefront then has the row, without
+// barriers (100,000 x 1,024 bf16 296 us, 321 in 128 lanes), and where 1,024 lanes would have too few
+// registers; else one, which leaves room for more rows (65,536 x 4,096 804, 841 in 256 lanes).
+inline NormShape norm_grad_shape(int32_t cols, bool wide) {
     const int32_t blocks = (cols + 7) / 8;
     if (blocks > 64 && blocks <= 128)
-        return {64, 2};
+        return wide ? NormShape{128, 1} : NormShape{64, 2};
+    if (blocks > 512 && blocks <= 1024)
+        return wide ? NormShape{512, 2} : NormShape{1024, 1};
     int32_t lanes = 16;
-    while (lanes < 1024 && lanes < blocks)
+    while (lanes < 512 && lanes < blocks)
         lanes *= 2;
     return blocks <= lanes ? NormShape{lanes, 1} : NormShape{0, 0};
 }
@@ -54,8 +57,8 @@ inline NormShape norm_grad_shape(int32_t cols) {
 // Its workgroups, each of which adds up its rows to a partial result: as many as the chip holds at a time,
 // of fewer rows so many that each has eight, but not fewer than half of the chip holds (4,000 x 1,024 30 us
 // with as many as the chip holds, 20 with half of it; 1,000 x 2,048 24 and 17).
-inline int64_t norm_grad_groups(int64_t rows, int32_t cols) {
-    const int32_t lanes = norm_grad_shape(cols).lanes, threads = lanes <= 64 ? 256 : lanes;
+inline int64_t norm_grad_groups(int64_t rows, int32_t cols, bool wide) {
+    const int32_t lanes = norm_grad_shape(cols, wide).lanes, threads = lanes <= 64 ? 256 : lanes;
     const int64_t at_once = threads / lanes, need = (rows + at_once - 1) / at_once;
     const int64_t most = 256 * (int64_t)(1024 / threads);
     const int64_t half = 256 * (int64_t)(threads < 512 ? 512 / threads : 1);

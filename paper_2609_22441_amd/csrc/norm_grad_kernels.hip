@@ -46,8 +46,13 @@ __device__ __forceinline__ void norm_back(int norm, const float (&t)[kCols], con
 // elements as they were read, and vectors wait in LDS.
 // At the end the groups of lanes of a workgroup add up their sums in order. BIAS: with post's bias or the
 // sums of either bias. partial: [workgroups][kSums][padded columns].
+template <typename T, typename S, int B, bool BIAS>
+constexpr int grad_wavefronts() {                 // on a unit: with few registers spilled, or none
+    return B == 2 ? 2 : (BIAS ? 3 : 4) - (sizeof(T) == 4);
+}
+
 template <typename T, typename S, int L, int B, bool TAIL, bool BIAS>
-__global__ __launch_bounds__(L <= 64 ? kThreads : L, B == 2 ? 2 : BIAS ? 3 : 4) void row_grad_kernel(
+__global__ __launch_bounds__(L <= 64 ? kThreads : L, (grad_wavefronts<T, S, B, BIAS>())) void row_grad_kernel(
     NormGradArgs ga, float *partial, int64_t padded) {
     const NormArgs &a = ga.a;
     constexpr int kT = L <= 64 ? kThreads : L, kGroups = kT / L;
@@ -94,33 +99,40 @@ __global__ __launch_bounds__(L <= 64 ? kThreads : L, B == 2 ? 2 : BIAS ? 3 : 4) 
             to[i] = p ? held_block<TAIL>(row_of<E>(p, stride, row), col[i], a.cols, exchange[i])
                       : Raw<E>{};
     };
-    struct Held {
-        Raw<T> f[B], u[B], dh[B];
-        Raw<S> x[B], dy[B];
-    } next;
-    auto fetch_row = [&](int64_t row) {
-        fetch(next.f, T(), a.f, a.f_stride, row);
-        fetch(next.u, T(), a.gate, a.gate_stride, row);
-        fetch(next.x, S(), a.x, a.x_stride, row);
-        fetch(next.dh, T(), ga.dh, ga.dh_stride, row);
-        fetch(next.dy, S(), ga.dy, ga.dy_stride, row);
-    };
     // Three wavefronts on a unit have registers for a row in 16 bits on its way while the row before is
     // computed: layer norms of 50,000 x 512 bf16 94 us, 101 without; with a stream in 32 bits they have
     // not (131,072 x 128 79 us, 167 with it), nor have four wavefronts.
     constexpr bool kAhead = L <= 64 && B == 1 && BIAS && sizeof(S) == 2;
-    const int64_t step = (int64_t)gridDim.x * kGroups;
-    int64_t row = (int64_t)blockIdx.x * kGroups + group_of_lanes<L>();
-    if (kAhead && row < a.n)
-        fetch_row(row);
-    for (; row < a.n; row += step) {
-        if (!kAhead)
-            fetch_row(row);
-        Held held = next;
-        auto &f = held.f, &u = held.u, &dh = held.dh;
-        auto &x = held.x, &dy = held.dy;
-        if (kAhead && row + step < a.n)
-            fetch_row(row + step);
+    Raw<T> next_f[B], next_u[B], next_dh[B];
+    Raw<S> next_x[B], next_dy[B];
+    const int64_t first_row = (int64_t)blockIdx.x * kGroups + group_of_lanes<L>();
+    auto fetch_next = [&](int64_t row) {
+        fetch(next_f, T(), a.f, a.f_stride, row);
+        fetch(next_u, T(), a.gate, a.gate_stride, row);
+        fetch(next_x, S(), a.x, a.x_stride, row);
+        fetch(next_dh, T(), ga.dh, ga.dh_stride, row);
+        fetch(next_dy, S(), ga.dy, ga.dy_stride, row);
+    };
+    if (kAhead && first_row < a.n)
+        fetch_next(first_row);
+    for (int64_t row = first_row; row < a.n; row += (int64_t)gridDim.x * kGroups) {
+        Raw<T> f[B], u[B], dh[B];
+        Raw<S> x[B], dy[B];
+        if constexpr (kAhead) {
+            f[0] = next_f[0];
+            u[0] = next_u[0];
+            x[0] = next_x[0];
+            dh[0] = next_dh[0];
+            dy[0] = next_dy[0];
+            if (row + (int64_t)gridDim.x * kGroups < a.n)
+                fetch_next(row + (int64_t)gridDim.x * kGroups);
+        } else {
+            fetch(f, T(), a.f, a.f_stride, row);
+            fetch(u, T(), a.gate, a.gate_stride, row);
+            fetch(x, S(), a.x, a.x_stride, row);
+            fetch(dh, T(), ga.dh, ga.dh_stride, row);
+            fetch(dy, S(), ga.dy, ga.dy_stride, row);
+        }
 #pragma unroll
         for (int i = 0; i < B; ++i)
             settle(f[i], exchange[i]);
@@ -511,7 +523,7 @@ template <typename T, typename S, int L, int B = 1>
 hipError_t launch_rows(const NormGradArgs &g, hipStream_t stream) {
     const NormArgs &a = g.a;
     constexpr int kT = L <= 64 ? kThreads : L;
-    const int64_t padded = padded_cols(a.cols), groups = norm_grad_groups(a.n, a.cols);
+    const int64_t padded = padded_cols(a.cols), groups = norm_grad_groups(a.n, a.cols, sizeof(S) == 4);
     float *partial = static_cast<float *>(g.workspace);
     auto even = [](const void *p, int64_t stride) { return !p || even_rows(p, stride); };
     const bool tail = !(a.cols % kCols == 0 && even(a.f, a.f_stride) && even(a.x, a.x_stride) &&
@@ -534,15 +546,25 @@ hipError_t launch_rows(const NormGradArgs &g, hipStream_t stream) {
 
 template <typename T, typename S>
 hipError_t launch_types(const NormGradArgs &g, hipStream_t stream) {
-    const NormShape shape = norm_grad_shape(g.a.cols);
+    constexpr bool kWideStream = sizeof(S) == 4;
+    const NormShape shape = norm_grad_shape(g.a.cols, kWideStream);
     switch (shape.lanes * 4 + shape.blocks) {
     case 16 * 4 + 1: return launch_rows<T, S, 16>(g, stream);
     case 32 * 4 + 1: return launch_rows<T, S, 32>(g, stream);
     case 64 * 4 + 1: return launch_rows<T, S, 64>(g, stream);
     case 256 * 4 + 1: return launch_rows<T, S, 256>(g, stream);
     case 512 * 4 + 1: return launch_rows<T, S, 512>(g, stream);
-    case 1024 * 4 + 1: return launch_rows<T, S, 1024>(g, stream);
-    case 64 * 4 + 2: return launch_rows<T, S, 64, 2>(g, stream);
+    }
+    if constexpr (kWideStream) {
+        if (shape.lanes == 128)
+            return launch_rows<T, S, 128>(g, stream);
+        if (shape.blocks == 2)
+            return launch_rows<T, S, 512, 2>(g, stream);
+    } else {
+        if (shape.lanes == 1024)
+            return launch_rows<T, S, 1024>(g, stream);
+        if (shape.blocks == 2)
+            return launch_rows<T, S, 64, 2>(g, stream);
     }
     const int64_t padded = padded_cols(g.a.cols), strips = norm_wide_strips(g.a.n, g.a.cols);
     RowStats *stats = static_cast<RowStats *>(g.workspace);
@@ -561,8 +583,10 @@ hipError_t launch_types(const NormGradArgs &g, hipStream_t stream) {
 }  // namespace
 
 int64_t norm_grad_workspace_bytes(int64_t n, int32_t cols) {
-    if (norm_grad_shape(cols).lanes)
-        return norm_grad_groups(n, cols) * kSums * padded_cols(cols) * 4;
+    if (norm_grad_shape(cols, false).lanes) {     // room for either type of the residual stream
+        const int64_t narrow = norm_grad_groups(n, cols, false), wide = norm_grad_groups(n, cols, true);
+        return (narrow > wide ? narrow : wide) * kSums * padded_cols(cols) * 4;
+    }
     return n * (int64_t)sizeof(RowStats) + norm_wide_strips(n, cols) * kSums * padded_cols(cols) * 4;
 }
 

@@ -19,10 +19,18 @@ SHIM = """#include "mx_choice.h"
 #include "norm_choice.h"
 extern "C" int norm(int32_t cols) { return ccj::norm_shape(cols).lanes * 4 + ccj::norm_shape(cols).blocks; }
 extern "C" int grad(int32_t cols) {
-    return ccj::norm_grad_shape(cols).lanes * 4 + ccj::norm_grad_shape(cols).blocks;
+    return ccj::norm_grad_shape(cols, false).lanes * 4 + ccj::norm_grad_shape(cols, false).blocks;
+}
+extern "C" int wide_grad(int32_t cols) {
+    return ccj::norm_grad_shape(cols, true).lanes * 4 + ccj::norm_grad_shape(cols, true).blocks;
 }
 extern "C" int64_t groups(int64_t rows, int32_t threads) { return ccj::norm_groups(rows, threads); }
-extern "C" int64_t grad_groups(int64_t rows, int32_t cols) { return ccj::norm_grad_groups(rows, cols); }
+extern "C" int64_t grad_groups(int64_t rows, int32_t cols) {
+    return ccj::norm_grad_groups(rows, cols, false);
+}
+extern "C" int64_t wide_grad_groups(int64_t rows, int32_t cols) {
+    return ccj::norm_grad_groups(rows, cols, true);
+}
 extern "C" int64_t strips(int64_t rows, int32_t cols) { return ccj::norm_wide_strips(rows, cols); }
 extern "C" int product(int64_t m, int64_t n, int64_t k) { return ccj::mx_product_choice(m, n, k); }
 extern "C" int inside(int64_t m, int64_t n, int64_t k) { return ccj::mx_quantize_inside(m, n, k); }
@@ -45,7 +53,7 @@ def choice():
     for name in ("product", "inside"):
         getattr(lib, name).argtypes = [ctypes.c_int64] * 3
     lib.lds.argtypes, lib.lds.restype = [ctypes.c_int64] * 2, ctypes.c_int64
-    for name in ("groups", "grad_groups", "strips"):
+    for name in ("groups", "grad_groups", "wide_grad_groups", "strips"):
         f = getattr(lib, name)
         f.argtypes, f.restype = [ctypes.c_int64, ctypes.c_int32], ctypes.c_int64
     return lib
@@ -89,7 +97,7 @@ def shapes(of):
 def test_norm_shapes_hold_their_rows(choice):
     """A row's lanes hold all of its blocks, and no fewer lanes of the same kernel would."""
     for cols in list(range(1, 16_385)) + [16_385, 1 << 24]:
-        for of, most in ((choice.norm, 16_384), (choice.grad, 8_192)):
+        for of, most in ((choice.norm, 16_384), (choice.grad, 8_192), (choice.wide_grad, 8_192)):
             lanes, blocks = divmod(of(cols), 4)
             assert (lanes == 0) == (cols > most)
             assert lanes == 0 or lanes * blocks * 8 >= cols
@@ -97,14 +105,15 @@ def test_norm_shapes_hold_their_rows(choice):
 
 def test_the_gpu_tests_reach_every_norm_kernel(choice):
     """Of each kernel, rows of whole blocks and others; and more rows than a launch goes through at once."""
-    for of in (choice.norm, choice.grad):
+    for of in (choice.norm, choice.grad, choice.wide_grad):
         for even in (True, False):
             assert {divmod(of(cols), 4) for _, cols in NORMS if (cols % 8 == 0) == even} == shapes(of)
-    for rows, cols in MANY_ROWS:
-        lanes = choice.grad(cols) // 4
-        threads = 256 if lanes <= 64 else lanes
-        assert rows > 2 * choice.grad_groups(rows, cols) * (threads // lanes)
-    assert {choice.grad(cols) // 4 for _, cols in MANY_ROWS} >= {16, 32, 64, 256, 512, 1024}
+    for of, groups in ((choice.grad, choice.grad_groups), (choice.wide_grad, choice.wide_grad_groups)):
+        for rows, cols in MANY_ROWS:
+            lanes = of(cols) // 4
+            threads = 256 if lanes <= 64 else lanes
+            assert rows > 2 * groups(rows, cols) * (threads // lanes)
+        assert {divmod(of(cols), 4) for _, cols in MANY_ROWS} == shapes(of) - {(0, 0)}
 
 
 def test_norm_launches_are_of_a_launchs_size(choice):
@@ -114,5 +123,6 @@ def test_norm_launches_are_of_a_launchs_size(choice):
             assert 1 <= n <= rows and n * threads < 1 << 32
         for cols in (1, 100, 1_000, 2_000, 4_000, 8_000):
             assert 1 <= choice.grad_groups(rows, cols) <= min(rows, 1_024)
+            assert 1 <= choice.wide_grad_groups(rows, cols) <= min(rows, 2_048)
         for cols in (9_000, 20_000, 1 << 24):
             assert 1 <= choice.strips(rows, cols) <= min(rows, 2_048)

@@ -156,10 +156,11 @@ def test_without_biases(rows, cols):
 def test_many_rows(rows, cols, weights):
     """More rows than a launch has groups of lanes."""
     note(f"block norm many rows {rows}x{cols}")
-    r = rng(rows)
-    c, t = make(r, rows, cols, post=O.LAYER, weights=weights)
-    check_forward(c, t, "bf16", "bf16", True)
-    check_grad(c, t, "bf16", "bf16", r, sums=weights)
+    for stream in ("bf16", "f32"):
+        r = rng(rows)
+        c, t = make(r, rows, cols, "bf16", stream, post=O.LAYER, weights=weights)
+        check_forward(c, t, "bf16", stream, True)
+        check_grad(c, t, "bf16", stream, r, sums=weights)
 
 
 def test_offsets_past_32_bits():

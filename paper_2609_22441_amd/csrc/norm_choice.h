@@ -7,10 +7,12 @@
 namespace ccj {
 
 // Lanes of a row, and blocks of 8 columns that each of them holds in registers; none: rows too long for
-// that, which go through the caches in pieces.
+// that, which go through the caches in pieces. Beyond a wavefront a row has as many as it needs.
 struct NormShape {
     int32_t lanes, blocks;
 };
+
+inline int32_t whole_wavefronts(int32_t lanes) { return (lanes + 63) / 64 * 64; }
 
 inline NormShape norm_shape(int32_t cols) {
     const int32_t blocks = (cols + 7) / 8;
@@ -19,13 +21,9 @@ inline NormShape norm_shape(int32_t cols) {
     if (blocks <= 128)
         return {64, 2};
     if (blocks <= 256)
-        return {256, 1};
-    if (blocks <= 512)
-        return {256, 2};
-    if (blocks <= 1024)
-        return {512, 2};
+        return {whole_wavefronts(blocks), 1};
     if (blocks <= 2048)
-        return {1024, 2};
+        return {whole_wavefronts((blocks + 1) / 2), 2};
     return {0, 0};
 }
 
@@ -41,17 +39,18 @@ inline int64_t norm_groups(int64_t rows, int32_t threads) {
 // The gradient's, which holds five matrices' elements and the sums over rows; wide: the residual stream is in
 // 32 bits, which leaves fewer registers. Two blocks a lane where one wavefront then has the row, without
 // barriers (100,000 x 1,024 bf16 296 us, 321 in 128 lanes), and where 1,024 lanes would have too few
-// registers; else one, which leaves room for more rows (65,536 x 4,096 804, 841 in 256 lanes).
+// registers; else one, which leaves room for more rows (65,536 x 4,096 804, 841 in 256 lanes). With a wide
+// stream the lanes are a power of two, known to the kernel: with any number of them it spilled more registers
+// (65,536 x 4,096 1,288 us, 1,047 so).
 inline NormShape norm_grad_shape(int32_t cols, bool wide) {
     const int32_t blocks = (cols + 7) / 8;
-    if (blocks > 64 && blocks <= 128)
-        return wide ? NormShape{128, 1} : NormShape{64, 2};
-    if (blocks > 512 && blocks <= 1024)
-        return wide ? NormShape{512, 2} : NormShape{1024, 1};
-    int32_t lanes = 16;
-    while (lanes < 512 && lanes < blocks)
-        lanes *= 2;
-    return blocks <= lanes ? NormShape{lanes, 1} : NormShape{0, 0};
+    if (blocks <= 64)
+        return {blocks <= 16 ? 16 : blocks <= 32 ? 32 : 64, 1};
+    if (blocks > 1024)
+        return {0, 0};
+    if (wide)
+        return blocks <= 512 ? NormShape{blocks <= 128 ? 128 : blocks <= 256 ? 256 : 512, 1} : NormShape{512, 2};
+    return blocks <= 128 ? NormShape{64, 2} : NormShape{whole_wavefronts(blocks), 1};
 }
 
 // Its workgroups, each of which adds up its rows to a partial result: as many as the chip holds at a time,

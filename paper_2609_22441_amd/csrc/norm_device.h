@@ -44,14 +44,22 @@ __device__ __forceinline__ float lanes_sum(float x) {
     return x;
 }
 
-// Sums of up to 2 numbers over the L lanes of a row, in each of them; of more than a wavefront through
-// LDS, whose two places take turns: a wavefront that writes to one again has passed a barrier that all
-// reached after they had read it.
-template <int L>
+// Sums of up to 2 numbers over the L lanes of a row, in each of them; of more than a wavefront, which are
+// the workgroup's and with FEWER possibly not all L, through LDS, whose two places take turns: a wavefront
+// that writes to one again has passed a barrier that all reached after they had read it. The places of
+// wavefronts that the workgroup does not have are 0.
+template <int L, bool FEWER = false>
 struct RowSum {
     static constexpr int kWaves = L > 64 ? L / 64 : 1;
     float (*place)[2][kWaves];
     int turn = 0;
+    __device__ __forceinline__ explicit RowSum(float (&p)[2][2][kWaves]) : place(p) {
+        if constexpr (L > 64 && FEWER) {
+            if (threadIdx.x < 4 * kWaves)
+                (&p[0][0][0])[threadIdx.x] = 0.0f;
+            __syncthreads();
+        }
+    }
     template <int N>
     __device__ __forceinline__ void operator()(float (&x)[N]) {
         static_assert(N <= 2, "");
@@ -267,7 +275,7 @@ __device__ __forceinline__ RowNorm norm_of(int kind, const float (&v)[B][kCols],
     return n;
 }
 
-// Number of a row that all lanes of a wavefront work on, where they do, as a scalar.
+// Which of a workgroup's rows a thread works on, as a scalar where all lanes of its wavefront do.
 template <int L>
 __device__ __forceinline__ int group_of_lanes() {
     const int group = threadIdx.x / L;

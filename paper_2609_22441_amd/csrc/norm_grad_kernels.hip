@@ -38,12 +38,13 @@ __device__ __forceinline__ void norm_back(int norm, const float (&t)[kCols], con
 // ---- rows in registers ----
 
 // L lanes of a row hold B blocks of 8 columns each, and for all the rows that they go through the sums over
-// rows of their columns. One read of f, gate, x, dy and dh, one write of dx, df and dgate; four sums over
-// the row's lanes one after another, two more with layer norms. Between these the vector units are what
-// is short (65,536 x 4,096 bf16: 750 instructions a lane and row were 55 % of their time at 1,226 us), so
-// that nothing is divided and no weight multiplied with scale for each row; and registers, of which a
-// wavefront may have 128 for four on a unit: what is behind one of the sums is computed again from the
-// elements as they were read, and vectors wait in LDS.
+// rows of their columns; with a stream in 16 bits and more than a wavefront L at most, the workgroup's. One
+// read of f, gate, x, dy and dh, one write of dx, df and dgate; four sums over the row's lanes one after
+// another, two more with layer norms. Between these the vector units are what is short (65,536 x 4,096 bf16:
+// 750 instructions a lane and row were 55 % of their time at 1,226 us), so that nothing is divided and no
+// weight multiplied with scale for each row; and registers, of which a wavefront may have 128 for four on a
+// unit: what is behind one of the sums is computed again from the elements as they were read, and vectors
+// wait in LDS.
 // At the end the groups of lanes of a workgroup add up their sums in order. BIAS: with post's bias or the
 // sums of either bias. partial: [workgroups][kSums][padded columns].
 template <typename T, typename S, int B, bool BIAS>
@@ -55,11 +56,12 @@ template <typename T, typename S, int L, int B, bool TAIL, bool BIAS>
 __global__ __launch_bounds__(L <= 64 ? kThreads : L, (grad_wavefronts<T, S, B, BIAS>())) void row_grad_kernel(
     NormGradArgs ga, float *partial, int64_t padded) {
     const NormArgs &a = ga.a;
-    constexpr int kT = L <= 64 ? kThreads : L, kGroups = kT / L;
+    constexpr int kGroups = L <= 64 ? kThreads / L : 1;
+    constexpr bool kFewer = L > 64 && sizeof(S) == 2;
     constexpr int kV = BIAS ? kSums : 2;          // of Sum, the biases come last
     __shared__ float place[2][2][L > 64 ? L / 64 : 1];
-    RowSum<L> sum{place};
-    const int lane = threadIdx.x % L;
+    RowSum<L, kFewer> sum(place);
+    const int lane = threadIdx.x % L, lanes = kFewer ? blockDim.x : L;
     const float per = 1.0f / (float)a.cols;
     int col[B], exchange[B];
     float w[B][kCols], sums[kV][B][kCols] = {};
@@ -77,8 +79,8 @@ __global__ __launch_bounds__(L <= 64 ? kThreads : L, (grad_wavefronts<T, S, B, B
     };
 #pragma unroll
     for (int i = 0; i < B; ++i) {
-        col[i] = (lane + i * L) * kCols;
-        exchange[i] = exchange_of(lane + i * L, a.cols);
+        col[i] = (lane + i * lanes) * kCols;
+        exchange[i] = exchange_of(lane + i * lanes, a.cols);
         vector_block(a.post_weight, col[i], a.cols, 1.0f, w[i]);
         times(w[i], a.scale);
         if (threadIdx.x < L)
@@ -282,7 +284,7 @@ __global__ __launch_bounds__(L <= 64 ? kThreads : L, (grad_wavefronts<T, S, B, B
                 for (int e = 0; e < kCols; ++e)
                     part[threadIdx.x / L][col[i] + e] = sums[v][i][e];
             __syncthreads();
-            for (int at = threadIdx.x; at < a.cols; at += kT) {
+            for (int at = threadIdx.x; at < a.cols; at += kThreads) {
                 float s = 0.0f;
 #pragma unroll
                 for (int g = 0; g < kGroups; ++g)
@@ -352,7 +354,7 @@ template <typename T, typename S>
 __global__ __launch_bounds__(kWide) void wide_stats_kernel(NormGradArgs ga, RowStats *stats) {
     const NormArgs &a = ga.a;
     __shared__ float place[2][2][kWide / 64];
-    RowSum<kWide> sum{place};
+    RowSum<kWide> sum(place);
     const float per = 1.0f / (float)a.cols;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         auto over = [&](auto &&use) {
@@ -520,9 +522,9 @@ hipError_t fold(const NormGradArgs &g, const float *partial, int64_t strips, hip
 }
 
 template <typename T, typename S, int L, int B = 1>
-hipError_t launch_rows(const NormGradArgs &g, hipStream_t stream) {
+hipError_t launch_rows(const NormGradArgs &g, int lanes, hipStream_t stream) {
     const NormArgs &a = g.a;
-    constexpr int kT = L <= 64 ? kThreads : L;
+    const int threads = L <= 64 ? kThreads : lanes;
     const int64_t padded = padded_cols(a.cols), groups = norm_grad_groups(a.n, a.cols, sizeof(S) == 4);
     float *partial = static_cast<float *>(g.workspace);
     auto even = [](const void *p, int64_t stride) { return !p || even_rows(p, stride); };
@@ -533,13 +535,13 @@ hipError_t launch_rows(const NormGradArgs &g, hipStream_t stream) {
     const bool bias = a.post_bias || g.sums[kPostBias] || g.sums[kPreBias];
     const unsigned grid = (unsigned)groups;
     if (tail && bias)
-        row_grad_kernel<T, S, L, B, true, true><<<grid, kT, 0, stream>>>(g, partial, padded);
+        row_grad_kernel<T, S, L, B, true, true><<<grid, threads, 0, stream>>>(g, partial, padded);
     else if (tail)
-        row_grad_kernel<T, S, L, B, true, false><<<grid, kT, 0, stream>>>(g, partial, padded);
+        row_grad_kernel<T, S, L, B, true, false><<<grid, threads, 0, stream>>>(g, partial, padded);
     else if (bias)
-        row_grad_kernel<T, S, L, B, false, true><<<grid, kT, 0, stream>>>(g, partial, padded);
+        row_grad_kernel<T, S, L, B, false, true><<<grid, threads, 0, stream>>>(g, partial, padded);
     else
-        row_grad_kernel<T, S, L, B, false, false><<<grid, kT, 0, stream>>>(g, partial, padded);
+        row_grad_kernel<T, S, L, B, false, false><<<grid, threads, 0, stream>>>(g, partial, padded);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? fold(g, partial, groups, stream) : e;
 }
@@ -549,22 +551,24 @@ hipError_t launch_types(const NormGradArgs &g, hipStream_t stream) {
     constexpr bool kWideStream = sizeof(S) == 4;
     const NormShape shape = norm_grad_shape(g.a.cols, kWideStream);
     switch (shape.lanes * 4 + shape.blocks) {
-    case 16 * 4 + 1: return launch_rows<T, S, 16>(g, stream);
-    case 32 * 4 + 1: return launch_rows<T, S, 32>(g, stream);
-    case 64 * 4 + 1: return launch_rows<T, S, 64>(g, stream);
-    case 256 * 4 + 1: return launch_rows<T, S, 256>(g, stream);
-    case 512 * 4 + 1: return launch_rows<T, S, 512>(g, stream);
+    case 16 * 4 + 1: return launch_rows<T, S, 16>(g, shape.lanes, stream);
+    case 32 * 4 + 1: return launch_rows<T, S, 32>(g, shape.lanes, stream);
+    case 64 * 4 + 1: return launch_rows<T, S, 64>(g, shape.lanes, stream);
     }
     if constexpr (kWideStream) {
-        if (shape.lanes == 128)
-            return launch_rows<T, S, 128>(g, stream);
-        if (shape.blocks == 2)
-            return launch_rows<T, S, 512, 2>(g, stream);
+        switch (shape.lanes * 4 + shape.blocks) {
+        case 128 * 4 + 1: return launch_rows<T, S, 128>(g, shape.lanes, stream);
+        case 256 * 4 + 1: return launch_rows<T, S, 256>(g, shape.lanes, stream);
+        case 512 * 4 + 1: return launch_rows<T, S, 512>(g, shape.lanes, stream);
+        case 512 * 4 + 2: return launch_rows<T, S, 512, 2>(g, shape.lanes, stream);
+        }
     } else {
-        if (shape.lanes == 1024)
-            return launch_rows<T, S, 1024>(g, stream);
         if (shape.blocks == 2)
-            return launch_rows<T, S, 64, 2>(g, stream);
+            return launch_rows<T, S, 64, 2>(g, shape.lanes, stream);
+        if (shape.lanes > 512)
+            return launch_rows<T, S, 1024>(g, shape.lanes, stream);
+        if (shape.lanes)
+            return launch_rows<T, S, 512>(g, shape.lanes, stream);
     }
     const int64_t padded = padded_cols(g.a.cols), strips = norm_wide_strips(g.a.n, g.a.cols);
     RowStats *stats = static_cast<RowStats *>(g.workspace);

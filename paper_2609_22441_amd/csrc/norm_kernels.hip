@@ -12,22 +12,23 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWide = 1024;                        // of rows of any length
 
-// Rows that stay in registers: L lanes of a row hold B blocks of 8 columns each, and weights and biases of
-// their columns for all the rows that they go through. One read of f, gate and x, one write of y and h; the
-// sums between them are over lanes, and over a workgroup's wavefronts through LDS. BIAS: with either bias.
+// Rows that stay in registers: the lanes of a row, L or beyond 64 all of a workgroup of at most L, hold B
+// blocks of 8 columns each, and weights and biases of their columns for all the rows that they go through.
+// One read of f, gate and x, one write of y and h; the sums between them are over lanes, and over a
+// workgroup's wavefronts through LDS. BIAS: with either bias.
 template <typename T, typename S, int L, int B, bool TAIL, bool BIAS>
 __global__ __launch_bounds__(L <= 64 ? kThreads : L) void row_norm_kernel(NormArgs a) {
-    constexpr int kT = L <= 64 ? kThreads : L, kGroups = kT / L;
+    constexpr int kGroups = L <= 64 ? kThreads / L : 1;
     __shared__ float place[2][2][L > 64 ? L / 64 : 1];
-    RowSum<L> sum{place};
-    const int lane = threadIdx.x % L;
+    RowSum<L, (L > 64)> sum(place);
+    const int lane = L > 64 ? threadIdx.x : threadIdx.x % L, lanes = L > 64 ? blockDim.x : L;
     const float per = 1.0f / (float)a.cols;
     int col[B], exchange[B];
     float post_w[B][kCols], post_b[B][kCols] = {}, pre_w[B][kCols], pre_b[B][kCols] = {};
 #pragma unroll
     for (int i = 0; i < B; ++i) {
-        col[i] = (lane + i * L) * kCols;
-        exchange[i] = exchange_of(lane + i * L, a.cols);
+        col[i] = (lane + i * lanes) * kCols;
+        exchange[i] = exchange_of(lane + i * lanes, a.cols);
         vector_block(a.post_weight, col[i], a.cols, 1.0f, post_w[i]);
         vector_block(a.pre_weight, col[i], a.cols, 1.0f, pre_w[i]);
         if (BIAS) {
@@ -93,7 +94,7 @@ __global__ __launch_bounds__(L <= 64 ? kThreads : L) void row_norm_kernel(NormAr
 template <typename T, typename S>
 __global__ __launch_bounds__(kWide) void wide_norm_kernel(NormArgs a) {
     __shared__ float place[2][2][kWide / 64];
-    RowSum<kWide> sum{place};
+    RowSum<kWide> sum(place);
     const float per = 1.0f / (float)a.cols;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         const T *f = row_of<T>(a.f, a.f_stride, row), *u = row_of<T>(a.gate, a.gate_stride, row);
@@ -164,35 +165,35 @@ __global__ __launch_bounds__(kWide) void wide_norm_kernel(NormArgs a) {
 }
 
 template <typename T, typename S, int L, int B>
-hipError_t launch_rows(const NormArgs &a, hipStream_t stream) {
-    constexpr int kT = L <= 64 ? kThreads : L, kGroups = kT / L;
-    const unsigned grid = (unsigned)norm_groups((a.n + kGroups - 1) / kGroups, kT);
+hipError_t launch_rows(const NormArgs &a, int lanes, hipStream_t stream) {
+    const int threads = L <= 64 ? kThreads : lanes, rows = L <= 64 ? kThreads / L : 1;
+    const unsigned grid = (unsigned)norm_groups((a.n + rows - 1) / rows, threads);
     const bool bias = a.post_bias || a.pre_bias;
     const bool even = a.cols % kCols == 0 && even_rows(a.f, a.f_stride) && even_rows(a.y, a.y_stride) &&
                       (!a.x || even_rows(a.x, a.x_stride)) && (!a.h || even_rows(a.h, a.h_stride)) &&
                       (!a.gate || even_rows(a.gate, a.gate_stride));
     if (even && bias)
-        row_norm_kernel<T, S, L, B, false, true><<<grid, kT, 0, stream>>>(a);
+        row_norm_kernel<T, S, L, B, false, true><<<grid, threads, 0, stream>>>(a);
     else if (even)
-        row_norm_kernel<T, S, L, B, false, false><<<grid, kT, 0, stream>>>(a);
+        row_norm_kernel<T, S, L, B, false, false><<<grid, threads, 0, stream>>>(a);
     else
-        row_norm_kernel<T, S, L, B, true, true><<<grid, kT, 0, stream>>>(a);
+        row_norm_kernel<T, S, L, B, true, true><<<grid, threads, 0, stream>>>(a);
     return hipGetLastError();
 }
 
 template <typename T, typename S>
 hipError_t launch_types(const NormArgs &a, hipStream_t stream) {
-    const NormShape shape = norm_shape(a.cols);
-    switch (shape.lanes * 4 + shape.blocks) {
-    case 16 * 4 + 1: return launch_rows<T, S, 16, 1>(a, stream);
-    case 32 * 4 + 1: return launch_rows<T, S, 32, 1>(a, stream);
-    case 64 * 4 + 1: return launch_rows<T, S, 64, 1>(a, stream);
-    case 64 * 4 + 2: return launch_rows<T, S, 64, 2>(a, stream);
-    case 256 * 4 + 1: return launch_rows<T, S, 256, 1>(a, stream);
-    case 256 * 4 + 2: return launch_rows<T, S, 256, 2>(a, stream);
-    case 512 * 4 + 2: return launch_rows<T, S, 512, 2>(a, stream);
-    case 1024 * 4 + 2: return launch_rows<T, S, 1024, 2>(a, stream);
-    }
+    const NormShape s = norm_shape(a.cols);
+    if (s.blocks == 1)
+        return s.lanes == 16   ? launch_rows<T, S, 16, 1>(a, s.lanes, stream)
+               : s.lanes == 32 ? launch_rows<T, S, 32, 1>(a, s.lanes, stream)
+               : s.lanes == 64 ? launch_rows<T, S, 64, 1>(a, s.lanes, stream)
+                               : launch_rows<T, S, 256, 1>(a, s.lanes, stream);
+    if (s.blocks == 2)
+        return s.lanes == 64    ? launch_rows<T, S, 64, 2>(a, s.lanes, stream)
+               : s.lanes <= 256 ? launch_rows<T, S, 256, 2>(a, s.lanes, stream)
+               : s.lanes <= 512 ? launch_rows<T, S, 512, 2>(a, s.lanes, stream)
+                                : launch_rows<T, S, 1024, 2>(a, s.lanes, stream);
     const int64_t most = 1 << 20;
     wide_norm_kernel<T, S><<<(unsigned)(a.n < most ? a.n : most), kWide, 0, stream>>>(a);
     return hipGetLastError();

@@ -19,11 +19,13 @@ INSIDE = [(1, 500, 32_768), (16, 640, 2_048), (13, 555, 2_400), (1, 16_384, 4_09
           (2, 9_000, 99)]
 OUTSIDE = [(1, 500, 32_769), (16, 640, 2_049), (1, 16_400, 96), (17, 64, 96), (16, 4_097, 2_048)]
 
-# Rows and columns of the norms: one column; part of a block of 8; rows for 16 lanes to 1,024; odd ends and
-# whole blocks of each; rows in pieces.
+# Rows and columns of the norms: one column; part of a block of 8; rows for 16 lanes to 1,024, wavefronts that
+# are no power of two among them; odd ends and whole blocks of each; rows in pieces.
 NORMS = [(1, 1), (3, 2), (5, 7), (70, 8), (33, 97), (40, 128), (37, 136), (29, 253), (21, 256), (19, 300),
-         (18, 512), (9, 520), (11, 1_003), (7, 1_024), (5, 1_032), (6, 2_047), (6, 2_048), (5, 2_051), (4, 4_096),
-         (3, 4_101), (3, 4_104), (3, 8_192), (2, 9_001), (2, 16_384), (2, 16_392), (3, 20_003), (2, 40_000)]
+         (18, 512), (9, 520), (11, 1_003), (7, 1_024), (5, 1_032), (5, 1_113), (6, 2_047), (6, 2_048), (5, 2_051),
+         (4, 2_344), (4, 4_096), (3, 4_101), (3, 4_104), (3, 5_000), (3, 6_093), (3, 8_192), (2, 9_001), (2, 9_680),
+         (2, 16_384), (2, 16_392), (3, 20_003), (2, 40_000)]
 
 # More rows than a launch has groups of lanes, several times.
-MANY_ROWS = [(17_000, 96), (9_000, 200), (5_000, 500), (9_000, 520), (2_100, 2_048), (700, 4_096), (600, 8_192)]
+MANY_ROWS = [(17_000, 96), (9_000, 200), (5_000, 500), (9_000, 520), (2_700, 1_300), (2_100, 2_048),
+             (700, 4_096), (600, 8_192)]

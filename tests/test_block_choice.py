@@ -90,8 +90,16 @@ def test_quantised_rows_fit_in_lds(choice):
         assert choice.inside(m, 16, k) and choice.lds(m, k) <= 48 << 10
 
 
-def shapes(of):
-    return {divmod(of(cols), 4) for cols in range(1, 20_000)}
+def kernel(of, cols, any_lanes=True):
+    """Lanes and blocks of a kernel: beyond a wavefront some take any number up to 256, 512 or 1,024."""
+    lanes, blocks = divmod(of(cols), 4)
+    if any_lanes and lanes > 64:
+        lanes = min(m for m in (256, 512, 1_024) if lanes <= m)
+    return lanes, blocks
+
+
+def kernels(of, any_lanes=True):
+    return {kernel(of, cols, any_lanes) for cols in range(1, 20_000)}
 
 
 def test_norm_shapes_hold_their_rows(choice):
@@ -105,20 +113,22 @@ def test_norm_shapes_hold_their_rows(choice):
 
 def test_the_gpu_tests_reach_every_norm_kernel(choice):
     """Of each kernel, rows of whole blocks and others; and more rows than a launch goes through at once."""
-    for of in (choice.norm, choice.grad, choice.wide_grad):
+    for of, any_lanes in ((choice.norm, True), (choice.grad, True), (choice.wide_grad, False)):
         for even in (True, False):
-            assert {divmod(of(cols), 4) for _, cols in NORMS if (cols % 8 == 0) == even} == shapes(of)
-    for of, groups in ((choice.grad, choice.grad_groups), (choice.wide_grad, choice.wide_grad_groups)):
+            reached = {kernel(of, cols, any_lanes) for _, cols in NORMS if (cols % 8 == 0) == even}
+            assert reached == kernels(of, any_lanes)
+    for of, groups, any_lanes in ((choice.grad, choice.grad_groups, True),
+                                  (choice.wide_grad, choice.wide_grad_groups, False)):
         for rows, cols in MANY_ROWS:
             lanes = of(cols) // 4
             threads = 256 if lanes <= 64 else lanes
             assert rows > 2 * groups(rows, cols) * (threads // lanes)
-        assert {divmod(of(cols), 4) for _, cols in MANY_ROWS} == shapes(of) - {(0, 0)}
+        assert {kernel(of, cols, any_lanes) for _, cols in MANY_ROWS} == kernels(of, any_lanes) - {(0, 0)}
 
 
 def test_norm_launches_are_of_a_launchs_size(choice):
     for rows in (1, 2, 3, 4, 2_047, 2_048, 10_000, 1 << 20, (1 << 31) - 1):
-        for threads in (256, 512, 1_024):
+        for threads in (128, 192, 256, 512, 1_024):
             n = choice.groups(rows, threads)
             assert 1 <= n <= rows and n * threads < 1 << 32
         for cols in (1, 100, 1_000, 2_000, 4_000, 8_000):

@@ -18,18 +18,23 @@ constexpr int32_t kMxTile256 = 3;        // 256 x 256
 
 constexpr int64_t kMxUnits = 256;        // compute units
 
-// 32 x 4,096 x 4,096 6.6 / 6.9, 1 x 8,192 x 16,384 14.6 / 23.2, 16 x 8,192 x 8,192 12.4 / 13.3; of more
-// tiles 33 x 4,096 x 4,096 7.9 / 6.9, 1 x 32,000 x 4,096 13.2 / 12.4.
+// 32 x 4,096 x 4,096 6.5 / 6.9, 1 x 8,192 x 16,384 14.2 / 23.3, 16 x 8,192 x 8,192 11.9 / 13.3; of more
+// tiles 33 x 4,096 x 4,096 7.9 / 6.9, 16 x 12,288 x 8,192 16.4 / 14.3, 48 x 4,096 x 8,192 15.9 / 13.1.
 constexpr int64_t kMxSkinnyTiles = 512;
 
 // A unit has two 64 x 64 tiles at a time: 512 x 4,096 x 16,384 38.8 / 45.8, 1,025 x 1,024 x 8,192 18.9 /
 // 24.2. A second round is too many: 512 x 8,192 x 4,096 23.3 / 16.0, 2,049 x 1,024 x 8,192 30.5 / 24.7.
 constexpr int64_t kMxTiles64 = 2 * kMxUnits;
 
+// Its wavefronts have a slab of 512 values of k each; of longer k two on their way, which takes registers: 4 x
+// 4,096 x 16,384 9.4 / 10.9, 1 x 2,048 x 65,536 23.6 / 27.7, the linear layer 1 x 8,192 x 8,192 9.4 / 12.7, but
+// 1 x 16,384 x 4,096, of one slab, 10.9 / 10.0.
+constexpr int64_t kMxOneSlab = 4096;
+
 // A linear layer's rows that the skinny kernel puts in 4 bits itself, every tile again: the values that a
-// unit's tiles take together. 1 x 4,096 x 4,096 4.4 / 6.8 (the next being a launch for them), 8 x 4,096 x
-// 4,096 6.3 / 7.4, 1 x 16,384 x 4,096 10.1 / 11.9, 1 x 4,096 x 32,768 20.8 / 24.1; of more values 16 x 4,096
-// x 4,096 8.7 / 7.8, 4 x 8,192 x 8,192 15.2 / 13.9, of more tiles 1 x 32,000 x 2,048 11.9 / 10.6.
+// unit's tiles take together. 1 x 4,096 x 4,096 4.2 / 7.0 (the next being a launch for them), 8 x 4,096 x
+// 4,096 6.1 / 6.9, 1 x 16,384 x 4,096 10.0 / 11.9, 1 x 8,192 x 8,192 9.4 / 11.1; of more values 16 x 4,096
+// x 4,096 8.7 / 7.4, 8 x 8,192 x 8,192 16.6 / 13.0, of more tiles 1 x 32,000 x 2,048 11.7 / 10.6.
 constexpr int64_t kMxInsideRows = 16, kMxInsideTiles = 1024, kMxInsideValues = 32768;
 
 // Short products of 256 x 256 tiles have their loads and stores on their own.

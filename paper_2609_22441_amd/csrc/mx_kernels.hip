@@ -569,14 +569,15 @@ constexpr int kSkinnyWaves = 8;
 // A workgroup has 16 x 16 results and its 8 wavefronts share out k, in slabs of 512 values; fragments
 // come from memory to registers as the matrix instruction takes them. A lane's four blocks of a slab
 // follow each other, 64 bytes and one word of scales; the sum over k may take its blocks in any order.
-// The wavefronts' sums meet in LDS.
+// The wavefronts' sums meet in LDS. TWO: two slabs of a wavefront are on their way at a time, for rows of
+// more than one slab each.
 //
 // QUANT: the rows of a (at most 16) are put in 4 bits from x in the kernel, by every workgroup again: a
 // few KiB from L2 on the weights' way, against a launch of their own.
-template <typename TO, bool QUANT>
+template <typename TO, bool QUANT, bool TWO>
 __global__ __launch_bounds__(64 * kSkinnyWaves) void skinny_kernel(MxProductArgs p, MxRowsArgs x,
                                                                    Divider div) {
-    constexpr int kSlab = 256, kT = 64 * kSkinnyWaves;           // bytes; threads
+    constexpr int kT = 64 * kSkinnyWaves, kSlab = 256, kStep = kSkinnyWaves * kSlab;   // threads; bytes
     extern __shared__ __attribute__((aligned(16))) uint8_t quantized[];
     __shared__ __attribute__((aligned(16))) float part[kSkinnyWaves][256];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -602,11 +603,16 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void skinny_kernel(MxProductArgs
         scale = *(const int *)(scales + at / 16);
         scale = k0 + piece < bytes ? scale : 0;
     };
-    int4_t fa[4], fb[4];
-    int scale_a, scale_b;
+    int4_t fa[4], fb[4], ga[4], gb[4];
+    int scale_fa, scale_fb, scale_ga, scale_gb;
     const int first = wave * kSlab;
+    auto read_b = [&](int k0) {
+        read(b, sb, fb, scale_fb, k0);
+        if (TWO && k0 + kStep < bytes)
+            read(b, sb, gb, scale_gb, k0 + kStep);
+    };
     if (first < bytes)
-        read(b, sb, fb, scale_b, first);
+        read_b(first);
     if constexpr (QUANT) {
         constexpr int kU = 4;                     // blocks of 8 columns of a thread on their way
         const int blocks = bytes / 4, units = (int)p.m * blocks;
@@ -633,14 +639,22 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void skinny_kernel(MxProductArgs
         __syncthreads();
     }
     float4_t acc = {};
-    for (int k0 = first; k0 < bytes; k0 += kSkinnyWaves * kSlab) {
+    auto add = [&](const int4_t (&x)[4], int scale_x, const int4_t (&y)[4], int scale_y) {
+        acc = multiply16<0>(x[0], y[0], acc, scale_x, scale_y);
+        acc = multiply16<1>(x[1], y[1], acc, scale_x, scale_y);
+        acc = multiply16<2>(x[2], y[2], acc, scale_x, scale_y);
+        acc = multiply16<3>(x[3], y[3], acc, scale_x, scale_y);
+    };
+    for (int k0 = first; k0 < bytes; k0 += (TWO ? 2 : 1) * kStep) {
+        const bool two = TWO && k0 + kStep < bytes;
         if (k0 != first)
-            read(b, sb, fb, scale_b, k0);
-        read(a, sa, fa, scale_a, k0);
-        acc = multiply16<0>(fb[0], fa[0], acc, scale_b, scale_a);
-        acc = multiply16<1>(fb[1], fa[1], acc, scale_b, scale_a);
-        acc = multiply16<2>(fb[2], fa[2], acc, scale_b, scale_a);
-        acc = multiply16<3>(fb[3], fa[3], acc, scale_b, scale_a);
+            read_b(k0);
+        read(a, sa, fa, scale_fa, k0);
+        if (two)
+            read(a, sa, ga, scale_ga, k0 + kStep);
+        add(fb, scale_fb, fa, scale_fa);
+        if (two)
+            add(gb, scale_gb, ga, scale_ga);
     }
     *(float4_t *)&part[wave][lane * 4] = acc;
     __syncthreads();
@@ -673,8 +687,8 @@ hipError_t launch_skinny(const MxProductArgs &p, hipStream_t stream) {
     const int64_t tiles = mx_tiles(p.m, p.n, 16, 16);
     if (tiles * (64 * kSkinnyWaves) > (int64_t)UINT32_MAX)
         return hipErrorInvalidConfiguration;
-    skinny_kernel<TO, false><<<(unsigned)tiles, 64 * kSkinnyWaves, 0, stream>>>(p, MxRowsArgs{},
-                                                                                Divider(1));
+    const auto kernel = p.k > kMxOneSlab ? skinny_kernel<TO, false, true> : skinny_kernel<TO, false, false>;
+    kernel<<<(unsigned)tiles, 64 * kSkinnyWaves, 0, stream>>>(p, MxRowsArgs{}, Divider(1));
     return hipGetLastError();
 }
 
@@ -696,8 +710,9 @@ template <typename T>
 hipError_t launch_linear_type(const MxRowsArgs &x, const MxProductArgs &p, hipStream_t stream) {
     if (mx_quantize_inside(p.m, p.n, p.k)) {
         const int64_t tiles = mx_tiles(p.m, p.n, 16, 16);
-        skinny_kernel<T, true><<<(unsigned)tiles, 64 * kSkinnyWaves, mx_quantize_lds(p.m, p.k),
-                                 stream>>>(p, x, Divider((uint32_t)(p.k / kCols)));
+        const auto kernel = p.k > kMxOneSlab ? skinny_kernel<T, true, true> : skinny_kernel<T, true, false>;
+        kernel<<<(unsigned)tiles, 64 * kSkinnyWaves, mx_quantize_lds(p.m, p.k), stream>>>(
+            p, x, Divider((uint32_t)(p.k / kCols)));
         return hipGetLastError();
     }
     const hipError_t e = quantize_type<T>(x, stream);

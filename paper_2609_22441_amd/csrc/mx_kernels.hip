@@ -682,21 +682,39 @@ hipError_t launch_tiles(const MxProductArgs &p, hipStream_t stream) {
     return hipGetLastError();
 }
 
+// Of rows that lie far apart there may be more tiles than a launch has room for: several launches then, of
+// as many columns as fit and of as many rows as these leave room for.
 template <typename TO>
-hipError_t launch_skinny(const MxProductArgs &p, hipStream_t stream) {
-    const int64_t tiles = mx_tiles(p.m, p.n, 16, 16);
-    if (tiles * (64 * kSkinnyWaves) > (int64_t)UINT32_MAX)
-        return hipErrorInvalidConfiguration;
-    const auto kernel = p.k > kMxOneSlab ? skinny_kernel<TO, false, true> : skinny_kernel<TO, false, false>;
-    kernel<<<(unsigned)tiles, 64 * kSkinnyWaves, 0, stream>>>(p, MxRowsArgs{}, Divider(1));
-    return hipGetLastError();
+hipError_t launch_skinny(const MxProductArgs &all, hipStream_t stream) {
+    const auto kernel = all.k > kMxOneSlab ? skinny_kernel<TO, false, true> : skinny_kernel<TO, false, false>;
+    const int64_t most = UINT32_MAX / (64 * kSkinnyWaves);       // tiles
+    for (int64_t n0 = 0; n0 < all.n; n0 += most * 16) {
+        MxProductArgs p = all;
+        p.n = all.n - n0 < most * 16 ? all.n - n0 : most * 16;
+        p.b = all.b + n0 * all.b_stride;
+        p.b_scales = all.b_scales + n0 * all.b_scales_stride;
+        p.bias = all.bias ? all.bias + n0 : nullptr;
+        const int64_t rows = most / mx_tiles(1, p.n, 16, 16) * 16;
+        for (int64_t m0 = 0; m0 < all.m; m0 += rows) {
+            p.m = all.m - m0 < rows ? all.m - m0 : rows;
+            p.a = all.a + m0 * all.a_stride;
+            p.a_scales = all.a_scales + m0 * all.a_scales_stride;
+            p.out = (char *)all.out + m0 * all.out_stride + n0 * (int64_t)sizeof(TO);
+            kernel<<<(unsigned)mx_tiles(p.m, p.n, 16, 16), 64 * kSkinnyWaves, 0, stream>>>(p, MxRowsArgs{},
+                                                                                          Divider(1));
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess)
+                return e;
+        }
+    }
+    return hipSuccess;
 }
 
 template <typename TO>
 hipError_t launch_product_type(const MxProductArgs &p, hipStream_t stream) {
     for (int64_t stride : {p.m > 1 ? p.a_stride : 0, p.n > 1 ? p.b_stride : 0,
                            p.m > 1 ? p.a_scales_stride : 0, p.n > 1 ? p.b_scales_stride : 0})
-        if (stride > kMaxStride)
+        if (p.k > 0 && stride > kMaxStride)       // rows of no columns: nothing is read
             return launch_skinny<TO>(p, stream);
     switch (mx_product_choice(p.m, p.n, p.k)) {
     case kMxSkinny: return launch_skinny<TO>(p, stream);

@@ -451,6 +451,14 @@ def _mx_width(k: int):
     return (k + 127) // 128 * 64, (k + 511) // 512 * 16
 
 
+def _of_width(x, name: str, width: int):
+    """As _matrix, of `width` columns also where that is 0."""
+    matrix = _matrix(x, name, width)
+    if matrix[3] != width:
+        _fail(name, f"needs {width} columns (shape {tuple(x.shape)})")
+    return matrix
+
+
 def _mx(L, q, scales, name: str, k=None, rows=None):
     """(pointer, row stride, scales' pointer and row stride, rows, k) of rows in 4 bits; of k values, or
     of as many as q has."""
@@ -462,9 +470,9 @@ def _mx(L, q, scales, name: str, k=None, rows=None):
         if k % 128:
             _fail(name, f"needs a multiple of 64 columns (shape {tuple(q.shape)})")
     width, scale_width = _mx_width(k)
-    p, stride, n, _ = _matrix(q, name, width)
+    p, stride, n, _ = _of_width(q, name, width)
     what = name + "_scales" if name != "q" else "scales"
-    ps, scale_stride, scale_rows, _ = _matrix(scales, what, scale_width)
+    ps, scale_stride, scale_rows, _ = _of_width(scales, what, scale_width)
     if rows is not None and n != rows:
         _fail(name, f"needs {rows} rows (shape {tuple(q.shape)})")
     if scale_rows != n:
@@ -517,7 +525,7 @@ def cc_matmul_mxfp4(a, a_scales, b, b_scales, out, bias=None, relu: bool = False
     pa, a_stride, pas, as_stride, m, k = _mx(L, a, a_scales, "a")
     pb, b_stride, pbs, bs_stride, n, _ = _mx(L, b, b_scales, "b", k)
     pbias = _b._arr(bias, "bias", L.f32, n, optional=True)
-    po, out_stride, out_rows, _ = _matrix(out, "out", n)
+    po, out_stride, out_rows, _ = _of_width(out, "out", n)
     if out_rows != m:
         _fail("out", f"needs {m} rows (shape {tuple(out.shape)})")
     t = _type(L, out, "out")
@@ -545,7 +553,7 @@ def cc_linear_mxfp4(x, w, w_scales, out, bias=None, relu: bool = False, workspac
     t = _type(L, x, "x")
     pw, w_stride, pws, ws_stride, n, _ = _mx(L, w, w_scales, "w", k)
     pbias = _b._arr(bias, "bias", L.f32, n, optional=True)
-    po, out_stride, out_rows, _ = _matrix(out, "out", n)
+    po, out_stride, out_rows, _ = _of_width(out, "out", n)
     if out_rows != m:
         _fail("out", f"needs {m} rows (shape {tuple(out.shape)})")
     if out.dtype != x.dtype:

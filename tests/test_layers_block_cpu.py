@@ -356,3 +356,35 @@ def test_quantisation_by_hand():
     assert list(codes[0, 32:35]) == [6, 1, 8 | 3]
     assert O.packed(codes)[0, 0] == 0x66
     assert list(O.values(codes, scales)[0, 32:35]) == [8.0, 1.0, -3.0]
+
+
+# ---- sizes of nothing ----
+
+@pytest.mark.parametrize("arg,bad,match", [
+    ("b", g(20, 64, dtype=U8), "0 columns"), ("b_scales", g(20, 16, dtype=U8), "0 columns"),
+    ("a_scales", g(10, 16, dtype=U8), "0 columns"), ("out", g(10, 21), "20 columns")])
+def test_a_product_of_no_columns_has_matrices_of_none(stub, arg, bad, match):
+    a = dict(a=g(10, 0, dtype=U8), a_scales=g(10, 0, dtype=U8), b=g(20, 0, dtype=U8),
+             b_scales=g(20, 0, dtype=U8), out=g(10, 20))
+    Y.cc_matmul_mxfp4(**a, stream=0)
+    assert [c[0] for c in stub.calls] == ["cc_matmul_mxfp4"]
+    a[arg] = bad
+    with pytest.raises(ValueError, match=match):
+        Y.cc_matmul_mxfp4(**a, stream=0)
+    assert len(stub.calls) == 1
+
+
+@pytest.mark.parametrize("name", ["cc_matmul_mxfp4", "cc_linear_mxfp4"])
+def test_a_product_with_no_rows_of_weights_has_an_output_of_no_columns(stub, name):
+    a = CALLS[name]()
+    weights = "b" if name == "cc_matmul_mxfp4" else "w"
+    a.update({weights: g(0, 320, dtype=U8), weights + "_scales": g(0, 32, dtype=U8), "bias": None,
+              "out": g(10, 0)})
+    if name == "cc_matmul_mxfp4":
+        a["out"] = g(10, 0, dtype=BF16)
+    getattr(Y, name)(**a, stream=0)
+    assert len(stub.calls) == 1
+    a["out"] = g(10, 20, dtype=a["out"].dtype)
+    with pytest.raises(ValueError, match="0 columns"):
+        getattr(Y, name)(**a, stream=0)
+    assert len(stub.calls) == 1

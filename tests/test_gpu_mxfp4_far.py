@@ -66,3 +66,29 @@ def test_more_tiles_than_a_launch_has(far):
         o = Output(*shape(64), torch.bfloat16)
         o.t.copy_(of(out, i, 64))
         check(o, *((want, size) if far == "b" else (want.t(), size.t())), 2, "bf16", f"rows from {i}")
+
+
+@pytest.mark.parametrize("m,n,k", [
+    (333, 1_030, 2_055),             # 64 x 64
+    (300, 9_001, 640),               # 128 x 128
+    (512, 32_768, 256)])             # 256 x 256
+@pytest.mark.parametrize("far", ["a", "b"])
+def test_offsets_of_a_tile_up_to_the_limit(m, n, k, far):
+    """Rows 2^24 bytes apart, the most that the tile kernels take: those of a tile lie up to 255 * 2^24 bytes
+    from its first, past 2^31. The same bits as of dense rows."""
+    note(f"mxfp4 far tiles {m}x{n}x{k} {far}")
+    if far == "b":
+        m, n = n, m
+    g = gen(m + k)
+    qa, sa, a = four_bits(g, m, k)
+    qb, sb, b = four_bits(g, n, k)
+    dense = torch.empty(m, n, device=DEV)
+    P.cc_matmul_mxfp4(qa, sa, qb, sb, dense)
+    if far == "a":
+        qa, sa = far_apart(qa, sa, STEP)
+    else:
+        qb, sb = far_apart(qb, sb, STEP)
+    o = Output(m, n, torch.float32)
+    P.cc_matmul_mxfp4(qa, sa, qb, sb, o.t)
+    assert torch.equal(o.t, dense)
+    check(o, a @ b.t(), a.abs() @ b.abs().t(), -(-k // 64), "f32", f"{m}x{n}x{k} {far}")

@@ -249,6 +249,23 @@ def test_the_native_path_makes_the_checks_call(case, monkeypatch):
 
 
 @pytest.mark.parametrize("case", range(8))
+def test_every_output_is_the_checks(case, monkeypatch):
+    """All tensors of a call but its workspace, those of 8 bits too."""
+    name = calls()[case][0]
+    note(f"marshal outputs: {name} {case}")
+    got = []
+    for path in (Y._load().marshal, B._ChecksOnly()):
+        name, args, kw, _ = calls()[case]
+        monkeypatch.setattr(Y._load(), "marshal", path)
+        getattr(P, name)(*args, **kw)
+        tensors = [t for i, t in enumerate(args) if not (name == "cc_block_norm_grad" and i == 2)]
+        got.append(tensors + [t for key, t in kw.items()
+                              if key != "workspace" and isinstance(t, torch.Tensor)])
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("case", range(8))
 def test_streams(case):
     """Work goes to the current stream, or to the one named by object or handle."""
     name, args, kw, at = calls()[case]

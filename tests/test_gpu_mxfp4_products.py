@@ -144,3 +144,24 @@ def test_rows_that_lie_far_apart():
     far_out = far_out.as_strided((m, 64), ((1 << 22) + 4, 1))
     P.cc_dequantize_mxfp4(q[:, :64], s[:, :16], far_out)
     assert torch.equal(far_out, out[:, :64])
+
+
+@pytest.mark.parametrize("m,n,k", [s for s in INSIDE if -(-s[0] // 16) * -(-s[1] // 16) <= 512] + OUTSIDE)
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_a_linear_layer_is_its_two_calls(m, n, k, dtype):
+    """Bit by bit where both take the same kernel: everywhere but at rows put in 4 bits within the product and
+    more than 512 tiles of 16 x 16, of which the product alone takes 64 x 64."""
+    note(f"mxfp4 linear as two calls {m}x{n}x{k} {dtype}")
+    g = gen(m + n + k)
+    x = torch.randn(m, k + 3, generator=g, device=DEV).to(TYPES[dtype])[:, :k]
+    w = torch.randn(n, k, generator=g, device=DEV)
+    room = [torch.empty(rows, -(-k // 128) * 64, dtype=torch.uint8, device=DEV) for rows in (m, n)]
+    scales = [torch.empty(rows, -(-k // 512) * 16, dtype=torch.uint8, device=DEV) for rows in (m, n)]
+    P.cc_quantize_mxfp4(x, room[0], scales[0])
+    P.cc_quantize_mxfp4(w, room[1], scales[1])
+    bias = torch.randn(n, generator=g, device=DEV)
+    one, two = (torch.empty(m, n, dtype=TYPES[dtype], device=DEV) for _ in range(2))
+    ws = torch.empty(P.cc_linear_mxfp4_workspace_bytes(m, n, k), dtype=torch.uint8, device=DEV)
+    P.cc_linear_mxfp4(x, room[1], scales[1], one, bias=bias, relu=True, workspace=ws)
+    P.cc_matmul_mxfp4(room[0], scales[0], room[1], scales[1], two, bias=bias, relu=True)
+    assert torch.equal(one, two)

@@ -116,7 +116,6 @@ int64_t norm_grad_workspace_bytes(int64_t n, int32_t cols);
 hipError_t launch_norm_grad(const NormGradArgs &a, hipStream_t stream);
 
 // Rows in microscaled 4-bit floating point.
-constexpr int32_t kMxBlock = 32;                  // values with one scale
 inline int64_t mx_padded(int64_t k) { return (k + 127) & ~(int64_t)127; }
 inline int64_t mx_scales(int64_t k) { return (k + 511) / 512 * 16; }       // bytes of a row's scales
 

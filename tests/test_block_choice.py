@@ -136,3 +136,15 @@ def test_norm_launches_are_of_a_launchs_size(choice):
             assert 1 <= choice.wide_grad_groups(rows, cols) <= min(rows, 2_048)
         for cols in (9_000, 20_000, 1 << 24):
             assert 1 <= choice.strips(rows, cols) <= min(rows, 2_048)
+
+
+def test_norm_gradients_have_no_more_workgroups_than_the_chip_has_room_for(choice):
+    """At any number of lanes: 1,024 threads a unit at most, none without a row; and no more partial results
+    than the workspace's documented bound, whatever the stream's type."""
+    for cols in list(range(1, 600)) + list(range(600, 8_193, 61)) + [1_032, 1_536, 2_048, 4_096, 8_192]:
+        for of, groups in ((choice.grad, choice.grad_groups), (choice.wide_grad, choice.wide_grad_groups)):
+            lanes = of(cols) // 4
+            threads = 256 if lanes <= 64 else lanes
+            for rows in (1, 2, 17, 999, 5_000, 131_072, (1 << 31) - 1):
+                n = groups(rows, cols)
+                assert 1 <= n <= min(-(-rows // (threads // lanes)), 256 * (1_024 // threads), 2_048)

@@ -234,7 +234,10 @@ CC_API cc_status cc_linear_i8(const void *x, int64_t x_stride, int32_t type, con
  *   n_rows      below 2^31; cols: 1 to 2^24.
  *   y           [n_rows][cols] of stream_type; h: [n_rows][cols] of `type`, or NULL.
  * In place: y may be x, and h may be f, where pointer and stride are the same.
- * Squares are summed in 32 bits: rows whose sum of squares passes 3.4e38 are not normalised.
+ * Squares are summed in 32 bits: rows whose sum of squares passes 3.4e38 are not normalised. Arithmetic
+ * is in 32 bits, with approximations of the hardware: inverse roots and reciprocals are within a unit
+ * in the last place, and exp(-|u|) of a sigmoid is off by up to |u| + 2 units, so that a gate at u = -80
+ * has a relative error of 1e-5. post's weight and bias are multiplied by scale before rows meet them.
  * Errors: CC_ERR_INVALID_ARGUMENT, CC_ERR_DEVICE.
  */
 CC_API cc_status cc_block_norm(const void *x, int64_t x_stride, int32_t stream_type, const void *f,
@@ -267,9 +270,9 @@ CC_API cc_status cc_block_norm(const void *x, int64_t x_stride, int32_t stream_t
  *   dx          [n_rows][cols] of stream_type, or NULL; df: [n_rows][cols] of `type`; dgate: the same,
  *               or NULL (it needs a gate).
  *   d_*         [cols] float, or NULL; d_pre_* need dh. Sums are in 32 bits in an order that
- *               depends on n_rows and cols alone: equal calls give equal bits. With `accumulate`
- *               they are added to what is there. A call with no rows writes zeros (accumulate:
- *               nothing).
+ *               depends on n_rows, cols and whether stream_type is CC_F32: equal calls give equal
+ *               bits. With `accumulate` they are added to what is there. A call with no rows
+ *               writes zeros (accumulate: nothing).
  *   workspace   cc_block_norm_grad_workspace_bytes(n_rows, cols) bytes.
  * Other arguments as in cc_block_norm. In place: dx may be dy, and df may be dh, where pointer and
  * stride are the same. Errors: CC_ERR_INVALID_ARGUMENT, CC_ERR_DEVICE.
@@ -331,8 +334,9 @@ CC_API cc_status cc_dequantize_mxfp4(const uint8_t *q, int64_t q_stride, const u
  *   out[i][j] = act(sum_l a[i][l] * b[j][l] + bias[j])
  *
  * a and b stand for the values that cc_dequantize_mxfp4 gives. Products are exact, their sum is in 32
- * bits in an order that depends on m, n and k alone; the result is rounded once. act as in
- * cc_matmul_i8.
+ * bits in an order that depends on m, n, k and whether a row stride passes 2^24 bytes: equal calls
+ * give equal bits, and a view of rows that lie further apart need not give those of its dense copy.
+ * The result is rounded once. act as in cc_matmul_i8.
  *
  *   a           [m][k / 2], row stride a_stride bytes; b: [n][k / 2], row stride b_stride bytes (a
  *               linear layer's weights, one row per output); a_scales: [m][16 * ceil(k / 512)],
@@ -358,6 +362,8 @@ CC_API cc_status cc_matmul_mxfp4(const uint8_t *a, int64_t a_stride, const uint8
 /*
  * cc_linear_mxfp4 -- cc_quantize_mxfp4 of x, then cc_matmul_mxfp4 with weights that are in 4 bits
  * already: a serving layer act(x W' + bias) on floating-point rows, in one call. It has no gradient.
+ * The order of its sums follows the same sizes and is not always cc_matmul_mxfp4's: of few rows the
+ * last bits may differ from those of the two calls.
  *
  *   x           [m][k] of `type`, row stride x_stride bytes, k from 1 to 2^24, any remainder.
  *   w, w_scales    [n] rows as cc_quantize_mxfp4 writes them from [n][k] weights.

@@ -1,10 +1,11 @@
 // Rows in microscaled 4-bit floating point: to 4 bits, back, and the product of two such matrices.
 //
 // To 4 bits and back are bound by memory: 16,384 x 8,192 bf16 59 us (339 MB, 5.8 TB/s) and 49 (339 MB, 6.9;
-// part of its input is in the caches). Large products are bound by power and by the way from L2 to LDS:
-// 16,384 x 8,192 x 8,192 515 us (4,270 TFLOP/s; matrix instructions on values in registers make 6,300), 8,192
-// x 16,384 x 4,096 280 (3,930, 268 MB of output follow the sums). Those of few rows by the launch and the weights' way: 1 x 4,096 x 4,096 with
-// the quantisation 4.4 us, 9.4 MB at 2.1 TB/s.
+// part of its input is in the caches). Large products are bound by power and by the way from L2 to LDS, as far
+// as an earlier step of the kernel with parts left out shows, and leave the matrix units idle while they
+// write: 16,384 x 8,192 x 8,192 515 us (4,270 TFLOP/s; matrix instructions on values in registers make 6,300),
+// 8,192 x 16,384 x 4,096 280 (3,930, 268 MB of output follow the sums). Those of few rows by the launch and
+// the weights' way: 1 x 4,096 x 4,096 with the quantisation 4.4 us, 9.4 MB at 2.1 TB/s.
 #include <type_traits>
 
 #include "layers_device.h"

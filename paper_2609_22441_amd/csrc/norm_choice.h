@@ -27,10 +27,11 @@ inline NormShape norm_shape(int32_t cols) {
     return {0, 0};
 }
 
-// Workgroups of the norm for `rows` rows or groups of rows that a workgroup takes at a time: as many as the
-// chip holds, and of more rows one for each four, which keeps the chip full to the end (65,536 x 4,096 bf16
-// 484 us, with as many as it holds 558) and still reads the weights once for four rows; a launch may not have
-// any number of them.
+// Workgroups of the norm for `rows` rows or groups of rows that a workgroup takes at a time: one each up to
+// 2,048 threads a unit (registers let a unit hold 512 to 2,048 of them at a time, the others follow), and of
+// more rows one for each four, which keeps the chip full to the end (65,536 x 4,096 bf16 484 us, with 2,048
+// threads a unit 558) and still reads the weights once for four rows; a launch may not have any number of
+// them.
 inline int64_t norm_groups(int64_t rows, int32_t threads) {
     const int64_t held = 256 * (int64_t)(2048 / threads), fours = (rows + 3) / 4, most = 1 << 20;
     return rows < held ? rows : fours < held ? held : fours < most ? fours : most;
@@ -53,9 +54,11 @@ inline NormShape norm_grad_shape(int32_t cols, bool wide) {
     return blocks <= 128 ? NormShape{64, 2} : NormShape{whole_wavefronts(blocks), 1};
 }
 
-// Its workgroups, each of which adds up its rows to a partial result: as many as the chip holds at a time,
-// of fewer rows so many that each has eight, but not fewer than half of the chip holds (4,000 x 1,024 30 us
-// with as many as the chip holds, 20 with half of it; 1,000 x 2,048 24 and 17).
+// Its workgroups, each of which adds up its rows to a partial result: up to 1,024 threads a unit, of fewer
+// rows so many that each has eight, but not fewer than half of that (4,000 x 1,024 30 us with 1,024 threads a
+// unit, 20 with half of them; 1,000 x 2,048 24 and 17). A unit holds 1,024 at a time of the kernels with four
+// wavefronts to a SIMD (grad_wavefronts in norm_grad_kernels.hip); of those with three or two, which biases,
+// 32-bit elements and two blocks a lane have, it holds 768 or 512, and the others follow in a second round.
 inline int64_t norm_grad_groups(int64_t rows, int32_t cols, bool wide) {
     const int32_t lanes = norm_grad_shape(cols, wide).lanes, threads = lanes <= 64 ? 256 : lanes;
     const int64_t at_once = threads / lanes, need = (rows + at_once - 1) / at_once;

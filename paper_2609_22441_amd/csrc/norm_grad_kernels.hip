@@ -37,6 +37,14 @@ __device__ __forceinline__ void norm_back(int norm, const float (&t)[kCols], con
 
 // ---- rows in registers ----
 
+// Wavefronts on a SIMD: with at most 15 registers of a lane spilled, but for rows beyond 4,096 columns, of
+// which kernels with biases spill 5 to 26 with a stream in 16 bits, 32 to 75 with one in 32, and those of
+// 32-bit elements without biases 16 to 22.
+template <typename T, typename S, int B, bool BIAS>
+constexpr int grad_wavefronts() {
+    return B == 2 ? 2 : (BIAS ? 3 : 4) - (sizeof(T) == 4);
+}
+
 // L lanes of a row hold B blocks of 8 columns each, and for all the rows that they go through the sums over
 // rows of their columns; with a stream in 16 bits and more than a wavefront L at most, the workgroup's. One
 // read of f, gate, x, dy and dh, one write of dx, df and dgate; four sums over the row's lanes one after
@@ -47,11 +55,6 @@ __device__ __forceinline__ void norm_back(int norm, const float (&t)[kCols], con
 // wait in LDS.
 // At the end the groups of lanes of a workgroup add up their sums in order. BIAS: with post's bias or the
 // sums of either bias. partial: [workgroups][kSums][padded columns].
-template <typename T, typename S, int B, bool BIAS>
-constexpr int grad_wavefronts() {                 // on a unit: with few registers spilled, or none
-    return B == 2 ? 2 : (BIAS ? 3 : 4) - (sizeof(T) == 4);
-}
-
 template <typename T, typename S, int L, int B, bool TAIL, bool BIAS>
 __global__ __launch_bounds__(L <= 64 ? kThreads : L, (grad_wavefronts<T, S, B, BIAS>())) void row_grad_kernel(
     NormGradArgs ga, float *partial, int64_t padded) {

@@ -165,3 +165,25 @@ def test_a_linear_layer_is_its_two_calls(m, n, k, dtype):
     P.cc_linear_mxfp4(x, room[1], scales[1], one, bias=bias, relu=True, workspace=ws)
     P.cc_matmul_mxfp4(room[0], scales[0], room[1], scales[1], two, bias=bias, relu=True)
     assert torch.equal(one, two)
+
+
+@pytest.mark.parametrize("m,n,k", [(16, 300, 640), (333, 1_030, 384), (300, 9_001, 256), (512, 32_768, 256)])
+def test_scales_at_both_ends(m, n, k):
+    """Rows with scales of 2^-127 to 2^127, of which products reach every size of 32 bits: scales of both are
+    taken together before anything is rounded, subnormal sums are kept. Each of the additions that `check`
+    counts is off by a unit of 2^-149 at least; sums beyond 2^126 may pass the type's end on their way."""
+    note(f"mxfp4 ends of scales {m}x{n}x{k}")
+    g = gen(m + n + k)
+    q, s, _ = zip(*(four_bits(g, rows, k) for rows in (m, n)))
+    for i, rows in enumerate((m, n)):
+        s[i].copy_(torch.randint(0, 255, (rows, 1), generator=g, device=DEV).to(torch.uint8).expand_as(s[i]))
+    a, b = (values(q[i], s[i]) for i in range(2))
+    want, size = a @ b.t(), a.abs() @ b.abs().t()
+    out = torch.empty(m, n, device=DEV)
+    P.cc_matmul_mxfp4(q[0], s[0], q[1], s[1], out)
+    steps = -(-k // 64) + 8
+    bound = (2 * steps + 1) * F32 * size + steps * TINY["f32"]
+    inside = size < 2.0 ** 126
+    assert bool(((out.double() - want).abs() <= bound)[inside].all())
+    small, middle = (size < 2.0 ** -126) & (want != 0), (size > 2.0 ** -20) & (size < 2.0 ** 20)
+    assert bool(small.any()) and bool(middle.any())
